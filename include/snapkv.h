@@ -386,6 +386,105 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The prompt's own attention (Sec. 4: the prompt phase that the compression follows; Sec. 4.1's window
+ * rows are its last queries): causal, grouped heads, a batch of sequences of different lengths stored
+ * one behind the other.  Its log-sum-exp rows are the lse_obs that snapkv_compress_lse, _strided,
+ * _grouped, _varlen and _paged take, so that scoring needs one sweep over K.
+ * Sequence b has Lq = q_lens[b] queries, the last ones of its Lk = k_lens[b] positions: query i sees
+ * the keys j <= Lk - Lq + i.  Lq = Lk is a whole prompt, Lq < Lk a chunk behind keys that are already
+ * there; with Lq > Lk the first Lq - Lk queries see nothing.
+ *   q            bf16 device, element(t, h, c) = q + t * q_strides[0] + h * q_strides[1] + c over all
+ *                sequences' tokens; k, v likewise with their strides and Hkv heads.  The strides are HOST
+ *                int64 [2] {token, head}, positive multiples of 8 below 2^39, at least d; NULL means
+ *                dense [tokens, heads, d].
+ *   q_lens       HOST int32 [B], >= 0.   k_lens  HOST int32 [B] or NULL (= q_lens).
+ *   q_starts     HOST int64 [B] or NULL: the first token of each sequence in q and in the outputs,
+ *                ascending and without overlap; NULL: one sequence behind the other.  k_starts likewise
+ *                for k and v (any order, overlaps allowed: common prefixes).
+ *   out          bf16 device, dense [tokens, Hq, d]: softmax_j(q_i.k_j / sqrt(d)) v_j
+ *   out_lse      fp32 device, dense [tokens, Hq], or NULL: natural log of sum_j exp(q_i.k_j / sqrt(d))
+ *   lse_obs      fp32 device, dense [B, Hq, W]: the same of each sequence's last W queries; NULL with
+ *                W = 0.  W <= 128, and with W > 0 every sequence needs W queries.
+ * A query that sees no key gets zeros and minus infinity.  Rows of q, out and out_lse that belong to no
+ * sequence are not touched; a sequence's keys and values reach its own queries only, whatever they hold.
+ * (Inside a sequence an infinity or NaN in a VALUE row may reach queries in front of it, too.)
+ * Products of bf16 accumulated in fp32, softmax statistics in fp32, probabilities rounded to bf16 for
+ * the product with V (they are at most 1 and their sum is taken before), results reproducible from run
+ * to run.  The host arrays are read during the call.  No workspace; one launch for every 32 sequences.
+ * A kernel wait that exceeds its limit makes the affected rows NaN.
+ */
+snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const void* v,
+                                         const int64_t* q_strides, const int64_t* k_strides,
+                                         const int64_t* v_strides, const int32_t* q_lens,
+                                         const int32_t* k_lens, const int64_t* q_starts,
+                                         const int64_t* k_starts, int B, int Hq, int Hkv, int d, int W,
+                                         void* out, float* out_lse, float* lse_obs, void* stream);
+
+/*
+ * Appends keys and values to a paged cache (the cache of Sec. 5.1.2's generation steps grows by one row
+ * per token), with the position rotation applied on the way, and rotates the queries that go with them.
+ *   k_new, v_new  bf16 device, element(b, i, h, c) = base + b * strides[0] + i * strides[1] +
+ *                 h * strides[2] + c with HOST int64 strides [3] {sequence, token, head}, positive
+ *                 multiples of 8 below 2^39, head and token strides at least d.
+ *   cu_tokens     device int32 [B + 1] or NULL.  NULL: every sequence has T / B tokens, addressed as
+ *                 above.  Otherwise packed: the tokens of sequence b are rows cu_tokens[b] ..
+ *                 cu_tokens[b + 1] - 1 of T rows (ascending, the first entry 0; the sequence stride is
+ *                 not used); rows from cu_tokens[B] on (a padded batch) belong to no sequence and are
+ *                 skipped, in q_out too.
+ *   cache_lens    device int32 [B]: rows that sequence b's cache holds before the call.  Its i-th new
+ *                 token becomes row cache_lens[b] + i: row r is row r % page_size of page
+ *                 page_table[b * pages_per_seq + r / page_size].
+ *   positions     device int32 [T] or NULL: the tokens' positions in the text, which compression makes
+ *                 differ from their cache rows.  NULL: the cache row.
+ *   inv_freq      device fp32 [rot / 2] or NULL (no rotation): pair r of a key is turned by the angle
+ *                 positions[t] * inv_freq[r] (product, reduction in 64 bits).  rot <= d is a multiple of
+ *                 16 (SNAPKV_ERR_UNSUPPORTED otherwise); elements from rot on are copied.  Pairs are (r, r + rot / 2), or with `interleaved`
+ *                 (2 r, 2 r + 1): (x, y) -> (x cos - y sin, x sin + y cos) in fp32, rounded once.
+ *   q             bf16 device or NULL, strides HOST [3] as for k_new; needs inv_freq.  q_out: bf16
+ *                 device, dense [T, Hq, d], the queries turned like the keys.
+ *   k_pool ...    the pools as in snapkv_compress_paged, written here, with Hc heads: cache head c gets
+ *                 key head c / (Hc / Hkv) (Hc = Hkv, or Hc = Hq for caches with one selection per
+ *                 query head).  Any page_size >= 1.
+ * With inv_freq = NULL this copies a dense compressed cache [B, Hc, rows, d] (strides {Hc * rows * d, d,
+ * rows * d}) into pages.  A row beyond the table, or whose table entry lies outside [0, num_pages), is
+ * dropped.  Two tokens must not share a cache row.  All else in the pools stays as it is.
+ * One kernel, no workspace; T = 0 does nothing.
+ */
+snapkv_status_t snapkv_append_paged(const void* k_new, const void* v_new, const int64_t* k_new_strides,
+                                    const int64_t* v_new_strides, const int32_t* cu_tokens,
+                                    const int32_t* cache_lens, const int32_t* positions,
+                                    const float* inv_freq, int rot, int interleaved, const void* q,
+                                    const int64_t* q_strides, void* q_out, void* k_pool, void* v_pool,
+                                    const int64_t* k_strides, const int64_t* v_strides,
+                                    const int32_t* page_table, int pages_per_seq, int page_size,
+                                    int num_pages, int B, int T, int Hq, int Hkv, int Hc, int d,
+                                    void* stream);
+
+/*
+ * snapkv_decode_attention on a paged cache with a length per sequence: one new token of every sequence
+ * attends to rows 0 .. seq_lens[b] - 1 of its cache.
+ *   q_cur       bf16 device, dense [B, Hq, d]
+ *   k_pool ...  as in snapkv_compress_paged with Hc heads (Hc divides Hq, query head h reads cache head
+ *               h / (Hq / Hc)); page_size a multiple of 16.  A table entry outside [0, num_pages) reads
+ *               as rows of zeros.
+ *   seq_lens    DEVICE int32 [B]: rows of each cache, the new token's own among them; may change between
+ *               replays of a captured graph.  Clamped to [0, pages_per_seq * page_size]; a sequence
+ *               without rows gets zeros and a log-sum-exp of minus infinity.
+ *   out         fp32 device, dense [B, Hq, d];  out_lse fp32 device [B, Hq] or NULL.
+ * What lies in a page behind a sequence's last row is never used (it may be anything).  Accuracy and
+ * reproducibility as in snapkv_decode_attention.  `workspace`: device memory of
+ * snapkv_decode_paged_workspace_size bytes (0: arguments not acceptable), 256-byte aligned, nothing in it
+ * has to be initialised; calls that may overlap on the GPU need one each.  B * Hq <= 65535.
+ */
+size_t snapkv_decode_paged_workspace_size(int B, int Hq, int Hc, int d);
+snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_pool, const void* v_pool,
+                                    const int64_t* k_strides, const int64_t* v_strides,
+                                    const int32_t* page_table, int pages_per_seq, int page_size,
+                                    int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
+                                    float* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/*
  * A prompt sharded along its length (context parallelism).  The paper stops at what one GPU
  * holds (Sec. 5.1.1: 380K tokens; Sec. 6 leaves prompt processing aside); Eq. 1-2 decompose
  * over ranges of keys, which is what these four per-shard steps implement.  A shard holds

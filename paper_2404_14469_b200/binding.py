@@ -37,6 +37,7 @@ SYMBOLS = [
     "snapkv_selftest_withheld_partials",
     "snapkv_compress_paged",
     "snapkv_shard_lse", "snapkv_lse_merge", "snapkv_shard_votes", "snapkv_gather_range",
+    "snapkv_prefill_attention", "snapkv_append_paged", "snapkv_decode_paged_workspace_size", "snapkv_decode_paged",
 ]
 
 # entry points for the extension and the tests alone (csrc/snapkv_binding.h)
@@ -104,6 +105,16 @@ def lib() -> ctypes.CDLL:
     L.snapkv_decode_workspace_size.argtypes = [c_int] * 4
     L.snapkv_decode_attention.restype = c_int
     L.snapkv_decode_attention.argtypes = [c_vp] * 3 + [c_int] * 5 + [c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.snapkv_prefill_attention.restype = c_int
+    L.snapkv_prefill_attention.argtypes = [c_vp] * 3 + [p64] * 3 + [p32] * 2 + [p64] * 2 + [c_int] * 5 + [c_vp] * 4
+    L.snapkv_append_paged.restype = c_int
+    L.snapkv_append_paged.argtypes = ([c_vp] * 2 + [p64] * 2 + [c_vp] * 4 + [c_int] * 2 + [c_vp, p64] + [c_vp] * 3
+                                      + [p64] * 2 + [c_vp] + [c_int] * 9 + [c_vp])
+    L.snapkv_decode_paged_workspace_size.restype = c_sz
+    L.snapkv_decode_paged_workspace_size.argtypes = [c_int] * 4
+    L.snapkv_decode_paged.restype = c_int
+    L.snapkv_decode_paged.argtypes = ([c_vp] * 3 + [p64] * 2 + [c_vp] + [c_int] * 3 + [c_vp] + [c_int] * 4
+                                      + [c_vp] * 3 + [c_sz, c_vp])
     L.snapkv_pool_topk_workspace_size.restype = c_sz
     L.snapkv_pool_topk_workspace_size.argtypes = [c_int, c_int]
     L.snapkv_pool_topk.restype = c_int
@@ -343,6 +354,42 @@ def snapkv_decode_attention(q_cur, cache_k, cache_v, workspace=None, want_lse: b
     """q_cur bf16 [B, Hq, d], cache_k/v bf16 [B, Hc, rows, d] (CUDA, contiguous) ->
     (out fp32 [B, Hq, d], lse fp32 [B, Hq] or None, workspace)."""
     return (_native or _load_native()).decode(q_cur, cache_k, cache_v, workspace, want_lse)
+
+
+def snapkv_prefill_attention(q, k, v, q_lens, k_lens=None, window: int = 0, q_starts=None, k_starts=None,
+                             out=None, want_lse: bool = True):
+    """Causal attention of a batch of prompts, or of chunks of them: sequence b's q_lens[b] queries are the
+    last of its k_lens[b] (None: as many) positions.
+
+    q: bf16 CUDA [tokens, Hq, d], k, v [tokens, Hkv, d], views with contiguous rows (other strides multiples
+    of 8 elements), sequences one behind the other or at q_starts / k_starts (lists of first tokens;
+    q_starts ascending, without overlap).  Returns (out bf16 [tokens, Hq, d], lse fp32 [tokens, Hq] or
+    None, lse_obs fp32 [B, Hq, window] or None): lse_obs is what the compression of the same prompts
+    takes.  Rows of no sequence are zeros (lse: minus infinity), or with `out` given (dense bf16
+    [tokens, Hq, d], written in place) left as they were in it."""
+    return (_native or _load_native()).prefill(q, k, v, q_lens, k_lens, window, q_starts, k_starts, out, want_lse)
+
+
+def snapkv_append_paged(k_new, v_new, k_pool, v_pool, page_table, cache_lens, cu_tokens=None, positions=None,
+                        inv_freq=None, interleaved: bool = False, q=None, q_out=None):
+    """Writes new keys and values behind the cache_lens[b] rows of each sequence's paged cache, turned by
+    their positions when inv_freq (fp32 CUDA [rot / 2]) is given, and returns the queries q turned likewise
+    (bf16 [tokens, Hq, d]; None without q).
+
+    k_new, v_new (and q): bf16 CUDA [tokens, Hkv, d] with cu_tokens (int32 CUDA [B + 1]), or [B, n, Hkv, d];
+    any strides with contiguous rows.  k_pool, v_pool: [num_pages, Hc, page_size, d] views as in
+    snapkv_compress_paged, written in place, Hc a multiple of Hkv.  cache_lens: int32 CUDA [B]; positions:
+    int32 CUDA, one per token (None: the row in the cache).  Tokens from cu_tokens[B] on are skipped, in
+    q_out too (undefined there in a fresh one)."""
+    return (_native or _load_native()).append(k_new, v_new, k_pool, v_pool, page_table, cache_lens, cu_tokens,
+                                              positions, inv_freq, interleaved, q, q_out)
+
+
+def snapkv_decode_paged(q_cur, k_pool, v_pool, page_table, seq_lens, workspace=None, want_lse: bool = True):
+    """snapkv_decode_attention on a paged cache: q_cur bf16 [B, Hq, d], pools [num_pages, Hc, page_size, d],
+    page_table int32 [B, pages_per_seq], seq_lens int32 [B] (all CUDA) -> (out fp32 [B, Hq, d], lse fp32
+    [B, Hq] or None, workspace)."""
+    return (_native or _load_native()).decode_paged(q_cur, k_pool, v_pool, page_table, seq_lens, workspace, want_lse)
 
 
 def snapkv_window_scores_lse(q_obs, k, lse_obs, out_vote=None, workspace=None):
