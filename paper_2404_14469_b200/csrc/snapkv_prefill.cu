@@ -1,7 +1,21 @@
 // The prompt's own attention (the phase in front of the compression step): causal, grouped heads,
 // sequences of different lengths.  Per query i of a sequence with Lq queries and Lk keys:
 //   out_i = sum_j p_ij v_j / l_i,  p_ij = exp(s_ij - m_i),  s_ij = q_i.k_j / sqrt(d),  j <= Lk - Lq + i
-// with m_i the running maximum and l_i the running sum; lse_i = m_i + ln l_i.
+// with m_i a reference near the running maximum and l_i the running sum; lse_i = m_i + ln l_i.
+//
+// One work unit: two tiles of 128 query rows that share their keys.  Of a group's query heads the
+// largest power of two that divides the group is packed into a tile, (token, head) with the head
+// fastest: 32 tokens of 4 heads instead of 128 of one, so that a unit's two tiles need the same keys
+// but for a few.  Both products run on tcgen05 over 128 keys at a time:
+//   S = Q.K^T into TMEM; a warpgroup per tile reads it back, a query row per thread (maximum and sum
+//   need no shuffles), and writes P = exp2(S c - m) in bf16 over it; O += P.V with P as the operand in
+//   TMEM and O in TMEM to the end.
+// The reference m of a row moves only when the maximum has risen by more than 2^8 (or at the row's
+// first tile): then the thread rescales its row of O, which is still for as long as P is not handed
+// over.  P <= 2^8 loses nothing in bf16, and the rows of most tiles move nothing.
+// Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  Persistent: a block's next unit has its
+// keys on the way while the present one is written out.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -9,86 +23,437 @@
 
 #include "../../include/snapkv.h"
 #include "launch.cuh"
+#include "sm100_ptx.cuh"
 #include "snapkv_internal.h"
 
 namespace snapkv {
 namespace {
 
-constexpr int PF_MAX_SEQS = 32;  // sequences that share a launch
-constexpr int PF_WARPS = 8, PF_KEYS = 32;
+constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
+constexpr int PF_THREADS = 320;
+constexpr int PF_KEYS = 128;      // keys per tile
+constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
 
 struct PrefillSeq {
   int lq, lk;
-  long long q0, k0;  // first token
+  int unit0;      // the sequence's first unit
+  int batch;      // index in the caller's batch
+  long long q0;   // first token
 };
+template <int MAPS>
 struct PrefillSeqs {
-  PrefillSeq s[PF_MAX_SEQS];
+  CUtensorMap k[MAPS], v[MAPS];  // a sequence's own rows: what lies behind them reads as zeros
+  PrefillSeq s[MAPS];
 };
 struct PrefillArgs {
-  const __nv_bfloat16 *q, *k, *v;
-  long long qt, qh, kt, kh, vt, vh;
-  int Hq, g, W, b0;
-  float c2;
+  int Hq, g, W, nseq, units;
+  int pack_log2;       // query heads per tile
+  int head_packs;      // Hq >> pack_log2
+  float c2;            // log2(e) / sqrt(d)
+  unsigned long long wait_ns;
   __nv_bfloat16* out;
   float *lse, *lse_obs;
 };
 
-// One warp per query, one lane per key of a tile.
 template <int D>
-__global__ void __launch_bounds__(PF_WARPS * 32) prefill_kernel(const PrefillArgs a, const PrefillSeqs seqs) {
-  __shared__ float ks[PF_KEYS][D + 1], vs[PF_KEYS][D], qs[PF_WARPS][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
-  const PrefillSeq s = seqs.s[blockIdx.z];
-  const int i0 = blockIdx.x * PF_WARPS, i = i0 + warp;
-  if (i0 >= s.lq) return;
+struct PfSmem {
+  static constexpr int COLS = D / 64;
+  static constexpr int TILE = COLS * PF_BLOCK;          // one tile of Q, K or V
+  static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
+  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
+  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile s_full, p_full, pv_done, o_free, and drain
+  static constexpr int NBAR = 2 * STAGES + 2 + 8 + 1;
+  static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
+  static constexpr int DYN_BYTES = OFF_MISC + 16 + 1024;
+  static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// Wait for a copy or an MMA that is in flight, when the abort flag is set already.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+  const unsigned long long t0 = globaltimer_ns();
+  while (!mbar_try_wait(bar, parity))
+    if (globaltimer_ns() - t0 > limit_ns) return;
+}
+
+// What a block knows of a unit.
+struct Unit {
+  int seq, lq, batch;
+  int n0;         // keys in front of the first query (may be negative)
+  int head0;      // first query head
+  int token0;     // first token of tile 0
+  long long q0;
+  int nk[2];      // key tiles of each query tile
+  int most;
+};
+
+template <int D, int MAPS>
+__global__ void __launch_bounds__(PF_THREADS, 1)
+prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, const __grid_constant__ PrefillSeqs<MAPS> seqs) {
+  using SM = PfSmem<D>;
+  constexpr int COLS = SM::COLS, STAGES = SM::STAGES, TILE = SM::TILE;
+  constexpr int TMEM_O = 256;   // S (and P over it) of tile t at 128 t, O at TMEM_O + D t
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t q_s = sbase + SM::OFF_Q, kv_s = sbase + SM::OFF_KV, bar0 = sbase + SM::OFF_BAR;
+  auto bar_full = [&](int s) { return bar0 + 8u * s; };
+  auto bar_empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
+  const uint32_t bar_qf = bar0 + 8u * (2 * STAGES), bar_qe = bar_qf + 8u;
+  auto bar_s = [&](int t) { return bar_qe + 8u * (1 + t); };
+  auto bar_p = [&](int t) { return bar_qe + 8u * (3 + t); };
+  auto bar_pv = [&](int t) { return bar_qe + 8u * (5 + t); };
+  auto bar_of = [&](int t) { return bar_qe + 8u * (7 + t); };
+  const uint32_t bar_drain = bar_qe + 8u * 9;
+  volatile uint32_t* tmem_ptr_s = reinterpret_cast<volatile uint32_t*>(smem + SM::OFF_MISC);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    tma_prefetch_desc(&tmQ);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(bar_full(s), 1);
+      mbar_init(bar_empty(s), 1);
+    }
+    mbar_init(bar_qf, 1);
+    mbar_init(bar_qe, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(bar_s(t), 1);
+      mbar_init(bar_p(t), 4);
+      mbar_init(bar_pv(t), 1);
+      mbar_init(bar_of(t), 4);
+    }
+    mbar_init(bar_drain, 1);
+    *abort_s = 0;
+    *reinterpret_cast<volatile unsigned long long*>(abort_s + 1) = a.wait_ns;
+    mbar_fence_init();
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_s)), 512);
+    tmem_relinquish();
+  }
   pdl_wait();
-  const int last = s.lk - s.lq + min(i0 + PF_WARPS, s.lq) - 1;  // of the block's last query
-  const int mine = i < s.lq ? s.lk - s.lq + i : -1;
-  for (int c = lane; c < D; c += 32)
-    qs[warp][c] = i < s.lq ? __bfloat162float(a.q[(s.q0 + i) * a.qt + h * a.qh + c]) : 0.f;
-  float m = -INFINITY, l = 0.f, acc[D / 32] = {};
-  for (int j0 = 0; j0 <= last; j0 += PF_KEYS) {
-    __syncthreads();
-    for (int e = threadIdx.x; e < PF_KEYS * D; e += PF_WARPS * 32) {
-      const int r = e / D, c = e % D, j = j0 + r;
-      const bool in = j <= last;
-      ks[r][c] = in ? __bfloat162float(a.k[(s.k0 + j) * a.kt + (h / a.g) * a.kh + c]) : 0.f;
-      vs[r][c] = in ? __bfloat162float(a.v[(s.k0 + j) * a.vt + (h / a.g) * a.vh + c]) : 0.f;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_ptr_s;
+
+  const int tok_log2 = 7 - a.pack_log2, tile_tokens = 1 << tok_log2;
+  // The unit that the block takes in round r: the list begins with the longest, and every other round
+  // runs backwards, so that no block gets the longer one of every round.
+  auto unit_at = [&](int r, Unit* u) {
+    const int c = static_cast<int>(blockIdx.x), G = static_cast<int>(gridDim.x);
+    const int i = r * G + (r & 1 ? G - 1 - c : c);
+    if (i >= a.units) return false;
+    int s = 0;
+    while (s + 1 < a.nseq && i >= seqs.s[s + 1].unit0) ++s;
+    const PrefillSeq& q = seqs.s[s];
+    const int blocks = (q.lq + 2 * tile_tokens - 1) >> (tok_log2 + 1);
+    const int at = i - q.unit0, from_end = at / a.head_packs;
+    u->seq = s;
+    u->lq = q.lq;
+    u->batch = q.batch;
+    u->q0 = q.q0;
+    u->n0 = q.lk - q.lq;
+    u->head0 = (at - from_end * a.head_packs) << a.pack_log2;
+    u->token0 = (blocks - 1 - from_end) << (tok_log2 + 1);
+    for (int t = 0; t < 2; ++t) {
+      const int first = u->token0 + t * tile_tokens, last = min(first + tile_tokens, q.lq) - 1;
+      u->nk[t] = last < first ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
     }
-    __syncthreads();
-    float x = 0.f;
-    for (int c = 0; c < D; ++c) x = fmaf(qs[warp][c], ks[lane][c], x);
-    x = j0 + lane <= mine ? x * a.c2 : -INFINITY;
-    float mn = x;
-    for (int o = 16; o; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-    mn = fmaxf(fmaxf(mn, m), -1e30f);
-    const float corr = exp2f(m - mn), p = exp2f(x - mn);
-    m = mn;
-    l = l * corr + p;
-    for (int t = 0; t < D / 32; ++t) acc[t] *= corr;
-    for (int r = 0; r < PF_KEYS; ++r) {
-      const float pr = __shfl_sync(0xffffffffu, p, r);
-      if (pr != 0.f)
-        for (int t = 0; t < D / 32; ++t) acc[t] = fmaf(pr, vs[r][lane + 32 * t], acc[t]);
+    u->most = max(u->nk[0], u->nk[1]);
+    return true;
+  };
+  Unit u;
+
+  if (warp == 8) {
+    // ------------------------------------------------------------ TMA
+    if (elect_one()) {
+      int fill = 0, nq = 0;
+      bool ok = true;
+      for (int r = 0; ok && unit_at(r, &u); ++r) {
+        if (u.most == 0) continue;
+        const int kv = u.head0 / a.g;
+        auto load = [&](const CUtensorMap* m, int j) {
+          const int s = fill % STAGES;
+          if (!mbar_wait_thread(bar_empty(s), (fill / STAGES & 1) ^ 1, abort_s, 1)) return false;
+          mbar_expect_tx(bar_full(s), TILE);
+          for (int c = 0; c < COLS; ++c)
+            tma_load_3d(kv_s + s * TILE + c * PF_BLOCK, m, bar_full(s), c * 64, j * PF_KEYS, kv);
+          ++fill;
+          return true;
+        };
+        ok = mbar_wait_thread(bar_qe, (nq & 1) ^ 1, abort_s, 2);
+        if (!ok) break;
+        mbar_expect_tx(bar_qf, 2 * TILE);
+        for (int t = 0; t < 2; ++t)
+          for (int c = 0; c < COLS; ++c)
+            tma_load_3d(q_s + t * TILE + c * PF_BLOCK, &tmQ, bar_qf, c * 64, u.head0,
+                        static_cast<int>(u.q0) + u.token0 + t * tile_tokens);
+        ++nq;
+        for (int j = 0; ok && j < u.most; ++j) ok = load(&seqs.k[u.seq], j) && load(&seqs.v[u.seq], j);
+      }
+      if (*abort_s != 0) {  // never leave with copies in flight
+        if (nq) drain(bar_qf, (nq - 1) & 1, a.wait_ns);
+        for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
+      }
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ MMA
+    if (elect_one()) {
+      constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16(128, D) | UMMA_B_MN_MAJOR;
+      int use = 0, nq = 0, np[2] = {0, 0}, npv[2] = {0, 0}, no[2] = {0, 0};
+      bool ok = true;
+      auto full = [&](int i) { return mbar_wait_thread(bar_full(i % STAGES), i / STAGES & 1, abort_s, 3); };
+      auto scores = [&](int t, int i) {  // S of tile t with the keys of ring entry i
+        // P of the tile before lies over it: that product must be through
+        if (npv[t] > 0 && !mbar_wait_thread(bar_pv(t), (npv[t] - 1) & 1, abort_s, 4)) return false;
+        const uint64_t qd = umma_desc_k128(q_s + t * TILE), kd = umma_desc_k128(kv_s + (i % STAGES) * TILE);
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t at = static_cast<uint64_t>((k >> 2) * (PF_BLOCK >> 4) + (k & 3) * 2);
+          tc_mma_bf16(tmem + 128 * t, qd + at, kd + at, idesc_s, k != 0);
+        }
+        tc_commit(bar_s(t));
+        return true;
+      };
+      auto values = [&](int t, int i, bool first) {
+        if (!mbar_wait_thread(bar_p(t), np[t]++ & 1, abort_s, 5)) return false;
+        // (a unit's first product overwrites O: the unit before must have been read out)
+        if (first && !mbar_wait_thread(bar_of(t), (no[t]++ & 1) ^ 1, abort_s, 6)) return false;
+        const uint64_t vd = umma_desc_mn128(kv_s + (i % STAGES) * TILE, PF_BLOCK);
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < PF_KEYS / 16; ++k)
+          tc_mma_bf16_ts(tmem + TMEM_O + D * t, tmem + 128 * t + 8 * k, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o,
+                         !first || k != 0);
+        tc_commit(bar_pv(t));
+        ++npv[t];
+        return true;
+      };
+      for (int r = 0; ok && unit_at(r, &u); ++r) {
+        if (u.most == 0) continue;
+        ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7) && full(use);
+        for (int t = 0; ok && t < 2; ++t)
+          if (u.nk[t] > 0) ok = scores(t, use);
+        if (!ok) break;
+        tc_commit(bar_empty(use % STAGES));
+        if (u.most == 1) tc_commit(bar_qe);
+        for (int j = 0; ok && j < u.most; ++j, use += 2) {
+          const bool more = j + 1 < u.most;
+          ok = full(use + 1) && (!more || full(use + 2));
+          for (int t = 0; ok && t < 2; ++t) {
+            if (j < u.nk[t]) ok = values(t, use + 1, j == 0);
+            if (ok && j + 1 < u.nk[t]) ok = scores(t, use + 2);
+          }
+          if (!ok) break;
+          tc_commit(bar_empty((use + 1) % STAGES));
+          if (more) tc_commit(bar_empty((use + 2) % STAGES));
+          if (j + 2 == u.most) tc_commit(bar_qe);  // the unit's last use of its queries
+        }
+      }
+      if (*abort_s != 0) {
+        tc_commit(bar_drain);
+        drain(bar_drain, 0, a.wait_ns);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ softmax
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + TMEM_O + D * t;
+    const unsigned long long scale2 = pack2(a.c2, a.c2);
+    int ns = 0, npv = 0;
+    bool ok = true;
+    for (int r = 0; unit_at(r, &u); ++r) {
+      const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
+      const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
+      const int nk = u.nk[t];
+      const int jmax = u.n0 + min(token, u.lq - 1);             // the last key that the row sees
+      const int jfree = u.n0 + u.token0 + t * tile_tokens;      // every row of the tile sees keys up to here
+      float m = -INFINITY, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m)
+      for (int j = 0; ok && j < nk; ++j) {
+        ok = mbar_wait_warp(bar_s(t), ns++ & 1, abort_s, 8);
+        if (!ok) break;
+        tc_fence_after();
+        float v[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, v[c]);
+        tmem_wait_ld();
+        if (j * PF_KEYS + PF_KEYS - 1 > jfree) {
+          const int see = jmax - j * PF_KEYS;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[c][i] = 32 * c + i <= see ? v[c][i] : -INFINITY;
+        }
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          mx[c] = fmaxf(v[c][0], v[c][1]);
+#pragma unroll
+          for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(mx[c], fmaxf(v[c][i], v[c][i + 1]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c2;
+        // (a row that sees no key keeps minus infinity, with 0 as its reference in the differences)
+        const bool move = top > m + 8.f;
+        if (j > 0 && __any_sync(0xffffffffu, move)) {
+          const float f = move ? ex2_approx(m - top) : 1.f;  // O is still: its last product was through before S
+          l *= f;
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            tmem_ld32(o_at + 32 * c, o);
+            tmem_wait_ld();
+            uint32_t w[2][16];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i >> 4][i & 15] = __float_as_uint(o[i] * f);
+            tmem_st16(o_at + 32 * c, w[0]);
+            tmem_st16(o_at + 32 * c + 16, w[1]);
+          }
+        }
+        if (j == 0 || move) m = top;
+        const float neg = m == -INFINITY ? 0.f : -m;
+        const unsigned long long negm = pack2(neg, neg);
+        unsigned long long sum = 0ull;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const unsigned long long p = ex2_approx2(fma2(pack2(v[c][i], v[c][i + 1]), scale2, negm));
+            sum = add2(sum, p);
+            const float2 x = unpack2(p);
+            // to bf16, half a step of 2^-8 of a probability whose fp32 value is in the sum
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+            w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          tmem_st16(s_at + 16 * c, w);
+        }
+        const float2 both = unpack2(sum);
+        l += both.x + both.y;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p(t));
+        ++npv;
+      }
+      // ---- the tile's result
+      if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (npv - 1) & 1, abort_s, 9);
+      tc_fence_after();
+      const float inv = ok ? (l > 0.f ? 1.f / l : 0.f) : NAN;
+      const bool mine = token < u.lq;
+      const long long at = (u.q0 + token) * a.Hq + head;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float o[32];
+        if (ok && nk > 0) {
+          tmem_ld32(o_at + 32 * c, o);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        }
+        if (mine) {
+          uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + 32 * c);
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              // (a row without keys may have read what another unit left in O)
+              const float x = l > 0.f || !ok ? o[i + 2 * e] * inv : 0.f, y = l > 0.f || !ok ? o[i + 2 * e + 1] * inv : 0.f;
+              const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+              w[e] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            dst[i >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (ok && nk > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_of(t));
+      }
+      if (mine) {
+        const float e = ok ? (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY) : NAN;
+        if (a.lse) a.lse[at] = e;
+        const int w = token - (u.lq - a.W);
+        if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
+      }
     }
   }
-  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  if (i >= s.lq) return;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  const long long row = (s.q0 + i) * a.Hq + h;
-  for (int t = 0; t < D / 32; ++t) a.out[row * D + lane + 32 * t] = __float2bfloat16(acc[t] * inv);
-  if (lane == 0) {
-    const float e = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-    if (a.lse) a.lse[row] = e;
-    if (i >= s.lq - a.W)
-      a.lse_obs[(static_cast<long long>(a.b0 + blockIdx.z) * a.Hq + h) * a.W + i - (s.lq - a.W)] = e;
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
   }
+}
+
+template <int D, int MAPS>
+cudaError_t launch_prefill(const CUtensorMap& tmQ, const PrefillArgs& a, const PrefillSeqs<MAPS>& seqs, cudaStream_t stream) {
+  auto kernel = prefill_kernel<D, MAPS>;
+  constexpr int SMEM = PfSmem<D>::DYN_BYTES;
+  static DeviceOnce ready;
+  if (!ready.done()) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    ready.set();
+  }
+  const int grid = a.units < sm_count() ? a.units : sm_count();
+  return launch_pdl(kernel, dim3(grid), dim3(PF_THREADS), SMEM, stream, tmQ, a, seqs);
 }
 
 bool strides_ok(const int64_t* s, int d) {
   for (int i = 0; i < 2; ++i)
     if (s[i] < d || (s[i] & 7) || s[i] >= (1ll << 39)) return false;
   return true;
+}
+
+// What a call is about, apart from its sequences.
+struct PrefillCall {
+  const uint16_t *k, *v;
+  const int64_t *ks, *vs;
+  int Hkv, d;
+};
+struct SeqSpan {
+  int lq, lk, batch;
+  long long q0, k0;
+};
+
+template <int MAPS>
+cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ, const SeqSpan* span, int n, cudaStream_t stream) {
+  using u64 = unsigned long long;
+  PrefillSeqs<MAPS> seqs = {};
+  const int tok = 2 << (7 - a.pack_log2);
+  long long units = 0;
+  for (int i = 0; i < n; ++i) {
+    const SeqSpan& p = span[i];
+    seqs.s[i] = PrefillSeq{p.lq, p.lk, static_cast<int>(units), p.batch, p.q0};
+    units += static_cast<long long>((p.lq + tok - 1) / tok) * a.head_packs;
+    const u64 dims[3] = {static_cast<u64>(c.d), static_cast<u64>(p.lk > 0 ? p.lk : 1), static_cast<u64>(c.Hkv)};
+    const u64 ks[2] = {static_cast<u64>(c.ks[0]) * 2, static_cast<u64>(c.ks[1]) * 2},
+              vs[2] = {static_cast<u64>(c.vs[0]) * 2, static_cast<u64>(c.vs[1]) * 2};
+    const unsigned box[3] = {64, PF_KEYS, 1};
+    if (!encode_tensor_map(&seqs.k[i], c.k + p.k0 * c.ks[0], 3, dims, ks, box) ||
+        !encode_tensor_map(&seqs.v[i], c.v + p.k0 * c.vs[0], 3, dims, vs, box))
+      return cudaErrorInvalidValue;
+  }
+  if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
+  a.nseq = n;
+  a.units = static_cast<int>(units);
+  if (units == 0) return cudaSuccess;
+  return c.d == 128 ? launch_prefill<128, MAPS>(tmQ, a, seqs, stream) : launch_prefill<64, MAPS>(tmQ, a, seqs, stream);
 }
 
 }  // namespace
@@ -121,35 +486,47 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
     k_end = k0 + lk;
     if (q_end > MAX_TOKENS || k_end > MAX_TOKENS) return SNAPKV_ERR_INVALID_ARG;
   }
+  // (sizes beyond these would leave 32-bit coordinates and unit numbers)
   PrefillArgs a = {};
-  a.q = static_cast<const __nv_bfloat16*>(q);
-  a.k = static_cast<const __nv_bfloat16*>(k);
-  a.v = static_cast<const __nv_bfloat16*>(v);
-  a.qt = qs[0], a.qh = qs[1], a.kt = ks[0], a.kh = ks[1], a.vt = vs[0], a.vh = vs[1];
   a.Hq = Hq, a.g = Hq / Hkv, a.W = W;
+  while (a.pack_log2 < 6 && a.g % (2 << a.pack_log2) == 0) ++a.pack_log2;
+  a.head_packs = Hq >> a.pack_log2;
   a.c2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
+  a.wait_ns = wait_limit_setting();
   a.out = static_cast<__nv_bfloat16*>(out);
   a.lse = out_lse, a.lse_obs = lse_obs;
+  if (q_end == 0) return SNAPKV_OK;
+  CUtensorMap tmQ;
+  {
+    using u64 = unsigned long long;
+    const u64 dims[3] = {static_cast<u64>(d), static_cast<u64>(Hq), static_cast<u64>(q_end)};
+    const u64 strides[2] = {static_cast<u64>(qs[1]) * 2, static_cast<u64>(qs[0]) * 2};
+    const unsigned box[3] = {64, 1u << a.pack_log2, 128u >> a.pack_log2};
+    if (!encode_tensor_map(&tmQ, q, 3, dims, strides, box)) return SNAPKV_ERR_CUDA;
+  }
+  const PrefillCall c = {static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), ks, vs, Hkv, d};
   int64_t q_at = 0, k_at = 0;
   for (int b0 = 0; b0 < B; b0 += PF_MAX_SEQS) {
-    PrefillSeqs seqs = {};
-    const int n = B - b0 < PF_MAX_SEQS ? B - b0 : PF_MAX_SEQS;
-    int most = 0;
-    for (int i = 0; i < n; ++i) {
-      PrefillSeq& s = seqs.s[i];
-      s.lq = q_lens[b0 + i];
-      s.lk = k_lens ? k_lens[b0 + i] : s.lq;
-      s.q0 = q_starts ? q_starts[b0 + i] : q_at;
-      s.k0 = k_starts ? k_starts[b0 + i] : k_at;
-      q_at = s.q0 + s.lq;
-      k_at = s.k0 + s.lk;
-      if (s.lq > most) most = s.lq;
+    SeqSpan span[PF_MAX_SEQS];
+    int n = 0;
+    for (int b = b0; b < B && b < b0 + PF_MAX_SEQS; ++b) {
+      SeqSpan p;
+      p.lq = q_lens[b];
+      p.lk = k_lens ? k_lens[b] : p.lq;
+      p.batch = b;
+      p.q0 = q_starts ? q_starts[b] : q_at;
+      p.k0 = k_starts ? k_starts[b] : k_at;
+      q_at = p.q0 + p.lq;
+      k_at = p.k0 + p.lk;
+      if (p.lq == 0) continue;
+      int i = n++;  // the longest first
+      for (; i > 0 && span[i - 1].lk < p.lk; --i) span[i] = span[i - 1];
+      span[i] = p;
     }
-    if (most == 0) continue;
-    a.b0 = b0;
-    const dim3 grid((most + PF_WARPS - 1) / PF_WARPS, Hq, n);
-    const cudaError_t e = launch_pdl(d == 128 ? prefill_kernel<128> : prefill_kernel<64>, grid, dim3(PF_WARPS * 32), 0,
-                                     static_cast<cudaStream_t>(stream), a, seqs);
+    if (n == 0) continue;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = n == 1 ? run_set<1>(c, a, tmQ, span, n, st)
+                                 : (n <= 8 ? run_set<8>(c, a, tmQ, span, n, st) : run_set<PF_MAX_SEQS>(c, a, tmQ, span, n, st));
     if (e != cudaSuccess) return SNAPKV_ERR_CUDA;
   }
   return SNAPKV_OK;
