@@ -20,7 +20,8 @@ NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["snapkv_api.cu", "snapkv_score.cu", "snapkv_select.cu", "snapkv_select_cluster.cu", "snapkv_gather.cu",
            "snapkv_metrics.cu", "snapkv_decode.cu", "snapkv_score_ragged.cu", "snapkv_prefill.cu", "snapkv_append.cu",
            "snapkv_decode_paged.cu"]
-HEADERS = ["sm100_ptx.cuh", "score_kernel.cuh", "snapkv_internal.h", "launch.cuh", "snapkv_binding.h", os.path.join("..", "..", "include", "snapkv.h")]
+HEADERS = ["sm100_ptx.cuh", "score_kernel.cuh", "snapkv_internal.h", "launch.cuh", "snapkv_binding.h", "decode_mma.cuh",
+           os.path.join("..", "..", "include", "snapkv.h")]
 NATIVE_SOURCE = "native_binding.cpp"
 NATIVE_HEADERS = ["snapkv_binding.h", os.path.join("..", "..", "include", "snapkv.h")]
 

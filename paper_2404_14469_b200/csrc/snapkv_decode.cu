@@ -31,6 +31,7 @@
 #include <mutex>
 
 #include "../../include/snapkv.h"
+#include "decode_mma.cuh"
 #include "launch.cuh"
 #include "sm100_ptx.cuh"
 #include "snapkv_internal.h"
@@ -51,26 +52,6 @@ struct DecPair { static constexpr int WARPS = 4, STAGES = 3, CTAS = 2; };
 
 constexpr int tile_rows(int D) { return DEC_STAGE_BYTES / (4 * D); }
 
-__device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
@@ -88,38 +69,6 @@ __device__ __forceinline__ void st_peer_f(uint32_t addr, float v) {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
-// Transpose of an 8x8 matrix of 16-bit elements spread over the warp as an mma fragment.
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-
-// The first NT bf16 terms of x (each the rounding of what the terms before it leave), two
-// elements at a time (packed pairs for an mma operand).
-template <int NT>
-__device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&t)[NT]) {
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    t[i] = *reinterpret_cast<const uint32_t*>(&h);
-    x -= __low2float(h);
-    y -= __high2float(h);
-  }
-}
-
-// Warp-wide wait for a copy of this warp's ring; false when the time limit has passed.
-__device__ __forceinline__ bool wait_copy(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
-  for (int i = 0; i < 256; ++i)
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  const unsigned long long t0 = globaltimer_ns();
-  for (;;) {
-    for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if (__shfl_sync(0xffffffffu, globaltimer_ns() - t0 > limit_ns ? 1 : 0, 0)) return false;
-  }
-}
 
 // Grid: (CTAs per cluster, B * Hc, groups of DEC_HEADS query heads).  NH: 2, 4 or 8, at least the
 // query heads of a CTA; column n of an instruction belongs to head n % NH and, in the product

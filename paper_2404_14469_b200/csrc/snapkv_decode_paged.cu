@@ -1,71 +1,433 @@
 // One generation step's attention over a paged cache with a length per sequence:
 // out = softmax(q . K^T / sqrt(d)) V over rows 0 .. seq_lens[b] - 1 of every sequence.
+//
+// Bound by HBM: the cache is read once per group of query heads.  The arithmetic is decode_kernel's
+// (tiles of 16 rows of d = 128, or 32 of d = 64, through a TMA ring per warp; both products on
+// warp-level matrix instructions with the cache as the 16-row operand; fp32 probabilities in three
+// bf16 terms), the split another: the lengths are known on the device alone and differ, so all tiles
+// of all (sequence, cache head) units are laid end to end and cut into one equal share per block.  A
+// share that covers a unit writes its result; a unit that crosses shares leaves one partial (maximum,
+// sum, unnormalised output) per share, which a second kernel folds in the order of the shares: same
+// bits every run, no counters, nothing to clear.  A warp's ring runs on across units, so that the next
+// unit's tiles are on the way while the present one is merged.
+// What lies behind a sequence's last row may be anything: scores there are replaced and the values
+// zeroed in registers, in a unit's last tile alone.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
 #include "../../include/snapkv.h"
+#include "decode_mma.cuh"
 #include "launch.cuh"
+#include "sm100_ptx.cuh"
 #include "snapkv_internal.h"
 
 namespace snapkv {
 namespace {
 
-constexpr int DP_WARPS = 8;
+constexpr int DP_WARPS = 8, DP_STAGES = 2;
+constexpr int DP_STAGE_BYTES = 8192;          // K and V of one row tile
+constexpr int DP_BOX_ROWS = 16;               // rows per copy: a page holds a whole number of them
+constexpr int DP_HEADS = 8;                   // query heads of a unit
+constexpr int DP_THREADS = DP_WARPS * 32;
+constexpr int DP_MAX_GRID = MAX_GRID;
+
+constexpr int dp_tile_rows(int D) { return DP_STAGE_BYTES / (4 * D); }
 
 struct DecodePagedArgs {
-  const __nv_bfloat16 *q, *k, *v;
-  long long kp[3], vp[3];
+  const __nv_bfloat16* q;
   const int32_t *table, *seq_lens;
-  int pages_per_seq, page_size, num_pages, Hq, g;
+  int pages_per_seq, page_size, B, Hq, g;
+  int chunks;       // groups of up to DP_HEADS query heads per cache head
+  int units;        // units per sequence: cache heads * chunks
+  int grid;
   float c2;
+  unsigned long long wait_ns;
   float *out, *lse;
+  // workspace: tiles in front of each sequence [B + 1], then [2 * grid] partials of DP_HEADS *
+  // (D + 2) floats: of the unit that a share begins inside, of the one that it begins with
+  long long* prefix;
+  float* partials;
 };
 
-// A block per query head; a warp takes every DP_WARPS-th row, its lanes the elements.
-template <int D>
-__global__ void __launch_bounds__(DP_WARPS * 32) decode_paged_kernel(const DecodePagedArgs a) {
-  constexpr int E = D / 32;
-  __shared__ float ms[DP_WARPS], ls[DP_WARPS], os[DP_WARPS][D];
-  pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, c = h / a.g;
+__device__ __forceinline__ int rows_of(const DecodePagedArgs& a, int b) {
   const long long most = static_cast<long long>(a.pages_per_seq) * a.page_size;
-  const long long want = a.seq_lens[b];
-  const int n = static_cast<int>(want < 0 ? 0 : (want < most ? want : most));
-  float q[E], acc[E] = {}, m = -INFINITY, l = 0.f;
-  for (int e = 0; e < E; ++e) q[e] = __bfloat162float(a.q[static_cast<long long>(blockIdx.x) * D + lane + 32 * e]);
-  for (int r = warp; r < n; r += DP_WARPS) {
-    const int pg = r / a.page_size, row = r - pg * a.page_size;
-    const int page = a.table[static_cast<long long>(b) * a.pages_per_seq + pg];
-    const bool in = page >= 0 && page < a.num_pages;
-    const __nv_bfloat16 *kr = a.k + page * a.kp[0] + c * a.kp[1] + row * a.kp[2],
-                        *vr = a.v + page * a.vp[0] + c * a.vp[1] + row * a.vp[2];
-    float x = 0.f;
-    for (int e = 0; e < E; ++e) x = fmaf(q[e], in ? __bfloat162float(kr[lane + 32 * e]) : 0.f, x);
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    x *= a.c2;
-    const float mn = fmaxf(m, x), corr = exp2f(m - mn), p = exp2f(x - mn);
-    m = mn;
-    l = l * corr + p;
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(p, in ? __bfloat162float(vr[lane + 32 * e]) : 0.f, acc[e] * corr);
+  const int n = __ldg(a.seq_lens + b);
+  return n < 0 ? 0 : (n < most ? n : static_cast<int>(most));
+}
+
+// How many shares the tiles are cut into: one per block, but no fewer tiles than a block has warps.
+__host__ __device__ __forceinline__ int shares(long long total, int grid) {
+  const long long s = (total + DP_WARPS - 1) / DP_WARPS;
+  return s < grid ? static_cast<int>(s) : grid;
+}
+
+// A walk over the units of a share.
+struct Walk {
+  int b, n, tiles;       // sequence, its rows and tiles per unit
+  int unit;              // of the sequence
+  int t0, t1;            // the share's tiles of the unit
+  long long left;        // tiles of the share from t0 on
+};
+
+template <int D>
+__device__ __forceinline__ void walk_next(const DecodePagedArgs& a, Walk& w) {
+  w.left -= w.t1 - w.t0;
+  if (w.left <= 0) return;
+  if (++w.unit == a.units) {
+    w.unit = 0;
+    do {
+      w.n = rows_of(a, ++w.b);
+    } while (w.n == 0 && w.b + 1 < a.B);
+    w.tiles = (w.n + dp_tile_rows(D) - 1) / dp_tile_rows(D);
   }
-  for (int e = 0; e < E; ++e) os[warp][lane + 32 * e] = acc[e];
+  w.t0 = 0;
+  w.t1 = w.left < w.tiles ? static_cast<int>(w.left) : w.tiles;
+}
+
+template <int D, int NH>
+__global__ void __launch_bounds__(DP_THREADS, 1)
+decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const DecodePagedArgs a) {
+  constexpr int ROWS = dp_tile_rows(D);   // cache rows per stage
+  constexpr int HALVES = D / 64;          // 64-element (128-byte) column blocks of a row
+  constexpr int KS = D / 16;              // k-steps of S, and pairs of 8-column tiles of the output
+  constexpr int BOX = ROWS * 128;         // bytes of one column block of a tile
+  constexpr int PART = DP_HEADS * D;      // floats of a warp's partial output
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[DP_WARPS][DP_STAGES];
+  __shared__ float w_m[2][DP_WARPS][DP_HEADS], w_l[2][DP_WARPS][DP_HEADS];
+  __shared__ long long scan_s[DP_WARPS], start_s[2], total_s;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  float* parts = reinterpret_cast<float*>(smem + DP_WARPS * DP_STAGES * DP_STAGE_BYTES);  // [2][warp][head][D]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int gid = lane >> 2, tig = lane & 3;   // mma fragment coordinates
+  const uint32_t ring = smem_u32(smem) + warp * (DP_STAGES * DP_STAGE_BYTES);
+  const uint32_t bar = smem_u32(&bars[warp][0]);
+  pdl_launch_dependents();
   if (lane == 0) {
-    ms[warp] = m;
-    ls[warp] = l;
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+    for (int s = 0; s < DP_STAGES; ++s) mbar_init(bar + 8u * s, 1);
+    mbar_fence_init();
+    fence_proxy_async();
+  }
+  __syncwarp();
+  pdl_wait();  // everything above touched this block's shared memory only
+
+  // ---- the block's share.  Every thread adds up the tiles of its run of sequences.
+  const int run = (a.B + DP_THREADS - 1) / DP_THREADS, b_lo = min(static_cast<int>(threadIdx.x) * run, a.B),
+            b_hi = min(b_lo + run, a.B);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) mine += (rows_of(a, b) + ROWS - 1) / ROWS;
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) scan_s[warp] = upto;
+  __syncthreads();
+  long long before = upto - mine;
+  long long total = 0;
+  for (int w = 0; w < DP_WARPS; ++w) {
+    if (w < warp) before += scan_s[w];
+    total += scan_s[w];
+  }
+  if (blockIdx.x == 0) {  // for the second kernel
+    long long p = before;
+    for (int b = b_lo; b < b_hi; ++b) {
+      a.prefix[b] = p;
+      p += (rows_of(a, b) + ROWS - 1) / ROWS;
+    }
+    if (threadIdx.x == 0) a.prefix[a.B] = total;
+  }
+  total *= a.units;
+  const int S = shares(total, a.grid);
+  if (static_cast<int>(blockIdx.x) >= S) return;
+  const long long lo = static_cast<long long>(blockIdx.x) * total / S, hi = (static_cast<long long>(blockIdx.x) + 1) * total / S;
+  {
+    long long p = before * a.units;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const long long next = p + static_cast<long long>((rows_of(a, b) + ROWS - 1) / ROWS) * a.units;
+      if (p <= lo && lo < next) {
+        start_s[0] = b;
+        start_s[1] = lo - p;
+      }
+      p = next;
+    }
   }
   __syncthreads();
-  float M = -INFINITY, L = 0.f;
-  for (int w = 0; w < DP_WARPS; ++w) M = fmaxf(M, ms[w]);
-  for (int w = 0; w < DP_WARPS; ++w) L += ms[w] == -INFINITY ? 0.f : ls[w] * exp2f(ms[w] - M);
-  for (int e = threadIdx.x; e < D; e += DP_WARPS * 32) {
-    float o = 0.f;
-    for (int w = 0; w < DP_WARPS; ++w) o += ms[w] == -INFINITY ? 0.f : os[w][e] * exp2f(ms[w] - M);
-    a.out[static_cast<long long>(blockIdx.x) * D + e] = n > 0 ? o / L : 0.f;
+  Walk cur;
+  cur.b = static_cast<int>(start_s[0]);
+  cur.n = rows_of(a, cur.b);
+  cur.tiles = (cur.n + ROWS - 1) / ROWS;
+  cur.unit = static_cast<int>(start_s[1] / cur.tiles);
+  cur.t0 = static_cast<int>(start_s[1] - static_cast<long long>(cur.unit) * cur.tiles);
+  cur.left = hi - lo;
+  cur.t1 = cur.left < cur.tiles - cur.t0 ? cur.t0 + static_cast<int>(cur.left) : cur.tiles;
+
+  // ---- the warp's tiles: every DP_WARPS-th of each unit.  `ahead` is the next one to be requested;
+  // its page numbers are fetched when the one before is requested.
+  Walk ahead = cur;
+  int at = cur.t0 + warp, page[ROWS / DP_BOX_ROWS];
+  auto find_page = [&] {  // settles `ahead` on a tile (or behind the share) and fetches its page numbers
+    while (ahead.left > 0 && at >= ahead.t1) {
+      walk_next<D>(a, ahead);
+      at = ahead.t0 + warp;
+    }
+    if (ahead.left > 0)
+#pragma unroll
+      for (int i = 0; i < ROWS / DP_BOX_ROWS; ++i) {
+        const int r = at * ROWS + i * DP_BOX_ROWS;
+        const int pg = r / a.page_size;
+        page[i] = r < ahead.n ? __ldg(a.table + static_cast<long long>(ahead.b) * a.pages_per_seq + pg) : -1;
+      }
+  };
+  int issued = 0;
+  auto request = [&] {  // K and V of the tile at hand, then on to the next
+    if (ahead.left <= 0) return;
+    if (lane == 0) {
+      const uint32_t dst = ring + (issued % DP_STAGES) * DP_STAGE_BYTES, bs = bar + 8u * (issued % DP_STAGES);
+      const int head = ahead.unit / a.chunks;
+      mbar_expect_tx(bs, DP_STAGE_BYTES);
+#pragma unroll
+      for (int i = 0; i < ROWS / DP_BOX_ROWS; ++i) {
+        const int r = at * ROWS + i * DP_BOX_ROWS, row = r % a.page_size;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+          tma_load_4d(dst + h * BOX + i * (DP_BOX_ROWS * 128), &tmK, bs, h * 64, row, head, page[i]);
+          tma_load_4d(dst + (HALVES + h) * BOX + i * (DP_BOX_ROWS * 128), &tmV, bs, h * 64, row, head, page[i]);
+        }
+      }
+    }
+    __syncwarp();
+    ++issued;
+    at += DP_WARPS;
+    find_page();
+  };
+  find_page();
+  for (int s = 0; s < DP_STAGES; ++s) request();
+
+  constexpr int NT = (3 * NH + 7) / 8;          // instructions with V per 16 keys and dimensions
+  const int term0 = (2 * tig) / NH;             // this lane's columns carry terms term0, term0 + 8 / NH, ...
+  const int lrow_k = lane & 15, lchunk_k = lane >> 4;
+  const int lrow_v = (lane & 7) + ((lane >> 4) << 3), lchunk_v = (lane >> 3) & 1;
+  int n = 0, buf = 0;
+  bool failed = false;
+  for (; cur.left > 0; walk_next<D>(a, cur), buf ^= 1) {
+    const int head = cur.unit / a.chunks, h0 = (cur.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
+    // Q as the B operand: column gid is head h0 + gid % NH (zero beyond gc)
+    uint32_t qb[KS][2];
+    {
+      const int h = gid % NH;
+      const __nv_bfloat16* qh = a.q + (static_cast<size_t>(cur.b) * a.Hq + head * a.g + h0 + h) * D + 2 * tig;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          qb[k][i] = h < gc ? __ldg(reinterpret_cast<const uint32_t*>(qh + k * 16 + i * 8)) : 0u;
+    }
+    float acc[KS][4];  // dimensions 16 j + gid (+ 8) of columns 2 tig, 2 tig + 1
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of columns 2 tig + {0, 1}; l: this lane's keys
+    for (int t = cur.t0 + warp; t < cur.t1 && !failed; t += DP_WARPS) {
+      const int s = n % DP_STAGES;
+      if (!wait_copy(bar + 8u * s, (n / DP_STAGES) & 1, a.wait_ns)) {
+        failed = true;
+        // never leave with copies in flight
+        for (int i = n + 1; i < issued; ++i) wait_copy(bar + 8u * (i % DP_STAGES), (i / DP_STAGES) & 1, a.wait_ns);
+        break;
+      }
+      ++n;
+      const uint32_t kb = ring + s * DP_STAGE_BYTES, vb = kb + HALVES * BOX;
+#pragma unroll
+      for (int sub = 0; sub < ROWS / 16; ++sub) {
+        const int key0 = t * ROWS + sub * 16;
+        const int rk = sub * 16 + lrow_k, rv = sub * 16 + lrow_v;
+        float sc[2][4];  // two chains, even and odd k-steps
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[0][i] = sc[1][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          uint32_t x[4];
+          ldsm_x4(kb + (k >> 2) * BOX + rk * 128 + ((((k & 3) * 2 + lchunk_k) ^ (rk & 7)) << 4), x);
+          mma_16816(sc[k & 1], x[0], x[1], x[2], x[3], qb[k][0], qb[k][1]);
+        }
+        const bool whole = key0 + 16 <= cur.n;
+        float p[4];  // keys gid (0, 1) and gid + 8 (2, 3) of the lane's two columns
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          p[i] = whole || key0 + gid + (i >> 1) * 8 < cur.n ? (sc[0][i] + sc[1][i]) * a.c2 : -INFINITY;
+        float mx[2] = {fmaxf(p[0], p[2]), fmaxf(p[1], p[3])};
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
+          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
+        }
+        if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float mn = fmaxf(m[c], mx[c]);
+            const float corr = m[c] == -INFINITY ? 0.f : exp2f(m[c] - mn);  // (nothing summed yet: 0)
+            l[c] *= corr;
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+              acc[j][c] *= corr;
+              acc[j][c + 2] *= corr;
+            }
+            m[c] = mn;
+          }
+        }
+        // (a subtile past the last row, possible for 32-row tiles, has no key: p = 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = m[i & 1] == -INFINITY ? 0.f : exp2f(p[i] - m[i & 1]);
+        l[0] += p[0] + p[2];
+        l[1] += p[1] + p[3];
+        uint32_t lo3[3], hi3[3];  // terms of keys gid and gid + 8
+        split_bf16<3>(p[0], p[1], lo3);
+        split_bf16<3>(p[2], p[3], hi3);
+        uint32_t bt[NT][2];      // P^T as the B operand: keys 2 tig, + 1 (and 8 further on) of column gid
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const int term = term0 + i * (8 / NH);
+          bt[i][0] = transpose8(term == 0 ? lo3[0] : (term == 1 ? lo3[1] : (term == 2 ? lo3[2] : 0u)));
+          bt[i][1] = transpose8(term == 0 ? hi3[0] : (term == 1 ? hi3[1] : (term == 2 ? hi3[2] : 0u)));
+        }
+        uint32_t keep[2] = {0xffffffffu, 0xffffffffu};  // keys 2 tig, + 1 and 8 further on: rows that exist
+        if (!whole)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int key = key0 + 2 * tig + 8 * i;
+            keep[i] = (key < cur.n ? 0xffffu : 0u) | (key + 1 < cur.n ? 0xffff0000u : 0u);
+          }
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          uint32_t x[4];
+          ldsm_x4_trans(vb + (j >> 2) * BOX + rv * 128 + ((((j & 3) * 2 + lchunk_v) ^ (rv & 7)) << 4), x);
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            mma_16816(acc[j], x[0] & keep[0], x[1] & keep[0], x[2] & keep[1], x[3] & keep[1], bt[i][0], bt[i][1]);
+        }
+      }
+      __syncwarp();  // every lane has read the stage
+      request();
+    }
+    if (failed) l[0] = l[1] = NAN;  // the outputs of this unit and of those behind it become NaN
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
+      l[1] += __shfl_xor_sync(0xffffffffu, l[1], o);
+    }
+    // the columns of one head (its terms) are NH apart: NH / 2 lanes
+#pragma unroll
+    for (int o = NH / 2; o < 4; o <<= 1)
+#pragma unroll
+      for (int j = 0; j < KS; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] += __shfl_xor_sync(0xffffffffu, acc[j][i], o);
+
+    // ---- merge the warps, in order (two buffers: a warp may run ahead into the next unit)
+    float* part = parts + buf * (DP_WARPS * PART);
+    if (tig < NH / 2) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int h = 2 * tig + c;
+        if (gid == 0) {
+          w_m[buf][warp][h] = failed ? 0.f : m[c];
+          w_l[buf][warp][h] = l[c];
+        }
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          part[(warp * DP_HEADS + h) * D + 16 * j + gid] = acc[j][c];
+          part[(warp * DP_HEADS + h) * D + 16 * j + gid + 8] = acc[j][c + 2];
+        }
+      }
+    }
+    __syncthreads();
+    const bool complete = cur.t0 == 0 && cur.t1 == cur.tiles;
+    float* slot = a.partials + static_cast<size_t>(2 * blockIdx.x + (cur.t0 == 0)) * (DP_HEADS * (D + 2));
+    for (int e = threadIdx.x; e < gc * D; e += DP_THREADS) {
+      const int h = e / D;  // the same in all lanes (D is a multiple of 32): lane w weighs warp w's partial
+      const float wm = w_m[buf][lane % DP_WARPS][h];
+      float M = wm;
+#pragma unroll
+      for (int o = 1; o < DP_WARPS; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      const float f = wm == -INFINITY ? 0.f : exp2f(wm - M);
+      const float fl = f * w_l[buf][lane % DP_WARPS][h];
+      float o = 0.f, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < DP_WARPS; ++w) {
+        o += part[w * PART + e] * __shfl_sync(0xffffffffu, f, w);
+        L += __shfl_sync(0xffffffffu, fl, w);
+      }
+      if (complete) {
+        const size_t bh = static_cast<size_t>(cur.b) * a.Hq + head * a.g + h0 + h;
+        a.out[bh * D + e % D] = o / L;
+        if (a.lse && e % D == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
+      } else {
+        slot[2 * DP_HEADS + e] = o;
+        if (e % D == 0) {
+          slot[h] = M;
+          slot[DP_HEADS + h] = L;
+        }
+      }
+    }
   }
-  if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = n > 0 ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+// A block per query head: folds the partials of a unit that crosses shares, in their order.
+template <int D>
+__global__ void __launch_bounds__(D) decode_paged_join_kernel(const DecodePagedArgs a) {
+  pdl_wait();
+  const int b = blockIdx.x / a.Hq, hq = blockIdx.x - b * a.Hq, e = threadIdx.x;
+  const int c = hq / a.g, hg = hq - c * a.g, chunk = hg / DP_HEADS, h = hg - chunk * DP_HEADS;
+  const long long p0 = a.prefix[b], tiles = a.prefix[b + 1] - p0, total = a.prefix[a.B] * a.units;
+  const size_t bh = blockIdx.x;
+  if (tiles == 0) {  // a sequence without rows
+    a.out[bh * D + e] = 0.f;
+    if (a.lse && e == 0) a.lse[bh] = -INFINITY;
+    return;
+  }
+  const int S = shares(total, a.grid);
+  auto owner = [&](long long x) { return static_cast<int>(((x + 1) * S - 1) / total); };  // the largest c: c total / S <= x
+  const long long x0 = p0 * a.units + static_cast<long long>(c * a.chunks + chunk) * tiles;
+  const int first = owner(x0), last = owner(x0 + tiles - 1);
+  if (first == last) return;  // complete already
+  auto slot = [&](int s) { return a.partials + static_cast<size_t>(2 * s + (s == first)) * (DP_HEADS * (D + 2)); };
+  float M = -INFINITY, L = 0.f, o = 0.f;
+  for (int s = first; s <= last; ++s) M = fmaxf(M, __ldcg(slot(s) + h));
+#pragma unroll 4
+  for (int s = first; s <= last; ++s) {
+    const float* p = slot(s);
+    const float f = exp2f(__ldcg(p + h) - M);
+    L += __ldcg(p + DP_HEADS + h) * f;
+    o += __ldcg(p + 2 * DP_HEADS + h * D + e) * f;
+  }
+  a.out[bh * D + e] = o / L;
+  if (a.lse && e == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <int D, int NH>
+cudaError_t launch_decode_paged(const CUtensorMap& tmK, const CUtensorMap& tmV, const DecodePagedArgs& a, cudaStream_t stream) {
+  constexpr int SMEM = DP_WARPS * DP_STAGES * DP_STAGE_BYTES + 2 * DP_WARPS * DP_HEADS * D * 4 + 1024;
+  auto kernel = decode_paged_kernel<D, NH>;
+  static DeviceOnce ready;
+  if (!ready.done()) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    ready.set();
+  }
+  const cudaError_t e = launch_pdl(kernel, dim3(a.grid), dim3(DP_THREADS), SMEM, stream, tmK, tmV, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(decode_paged_join_kernel<D>, dim3(a.B * a.Hq), dim3(D), 0, stream, a);
 }
 
 bool strides_ok(const int64_t* s, int d) {
@@ -75,12 +437,22 @@ bool strides_ok(const int64_t* s, int d) {
   return s[2] >= d;
 }
 
+bool pool_map(CUtensorMap* m, const void* pool, const int64_t* s, int d, int page_size, int heads, int num_pages) {
+  using u64 = unsigned long long;
+  const u64 dims[4] = {static_cast<u64>(d), static_cast<u64>(page_size), static_cast<u64>(heads), static_cast<u64>(num_pages)};
+  const u64 strides[3] = {static_cast<u64>(s[2]) * 2, static_cast<u64>(s[1]) * 2, static_cast<u64>(s[0]) * 2};
+  const unsigned box[4] = {64, DP_BOX_ROWS, 1, 1};
+  return encode_tensor_map(m, pool, 4, dims, strides, box);
+}
+
 }  // namespace
 }  // namespace snapkv
 
 extern "C" size_t snapkv_decode_paged_workspace_size(int B, int Hq, int Hc, int d) {
+  using namespace snapkv;
   if (B < 1 || Hq < 1 || Hc < 1 || Hq % Hc != 0 || (d != 64 && d != 128)) return 0;
-  return 256;
+  return align256((static_cast<size_t>(B) + 1) * sizeof(long long)) +
+         align256(static_cast<size_t>(2) * DP_MAX_GRID * DP_HEADS * (d + 2) * sizeof(float));
 }
 
 extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_pool, const void* v_pool,
@@ -91,7 +463,7 @@ extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_
                                                void* stream) {
   using namespace snapkv;
   if (B < 1 || Hq < 1 || Hc < 1 || Hq % Hc != 0 || d < 1 || pages_per_seq < 1 || page_size < 1 || num_pages < 1 ||
-      page_size % 16 != 0)
+      page_size % DP_BOX_ROWS != 0)
     return SNAPKV_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || static_cast<long long>(B) * Hq > 65535 ||
       static_cast<long long>(pages_per_seq) * page_size >= (1ll << 31) - 64)
@@ -106,20 +478,24 @@ extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
       workspace_bytes < snapkv_decode_paged_workspace_size(B, Hq, Hc, d))
     return SNAPKV_ERR_WORKSPACE;
+  CUtensorMap tmK, tmV;
+  if (!pool_map(&tmK, k_pool, k_strides, d, page_size, Hc, num_pages) ||
+      !pool_map(&tmV, v_pool, v_strides, d, page_size, Hc, num_pages))
+    return SNAPKV_ERR_CUDA;
   DecodePagedArgs a = {};
   a.q = static_cast<const __nv_bfloat16*>(q_cur);
-  a.k = static_cast<const __nv_bfloat16*>(k_pool);
-  a.v = static_cast<const __nv_bfloat16*>(v_pool);
-  for (int i = 0; i < 3; ++i) {
-    a.kp[i] = k_strides[i];
-    a.vp[i] = v_strides[i];
-  }
   a.table = page_table, a.seq_lens = seq_lens;
-  a.pages_per_seq = pages_per_seq, a.page_size = page_size, a.num_pages = num_pages;
-  a.Hq = Hq, a.g = Hq / Hc;
+  a.pages_per_seq = pages_per_seq, a.page_size = page_size, a.B = B, a.Hq = Hq, a.g = Hq / Hc;
+  a.chunks = (a.g + DP_HEADS - 1) / DP_HEADS;
+  a.units = Hc * a.chunks;
+  a.grid = sm_count() < DP_MAX_GRID ? sm_count() : DP_MAX_GRID;
   a.c2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
+  a.wait_ns = wait_limit_setting();
   a.out = out, a.lse = out_lse;
-  const cudaError_t e = launch_pdl(d == 128 ? decode_paged_kernel<128> : decode_paged_kernel<64>, dim3(B * Hq),
-                                   dim3(DP_WARPS * 32), 0, static_cast<cudaStream_t>(stream), a);
-  return e == cudaSuccess ? SNAPKV_OK : SNAPKV_ERR_CUDA;
+  a.prefix = static_cast<long long*>(workspace);
+  a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256((static_cast<size_t>(B) + 1) * sizeof(long long)));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  auto f = d == 128 ? (a.g <= 2 ? launch_decode_paged<128, 2> : (a.g <= 4 ? launch_decode_paged<128, 4> : launch_decode_paged<128, 8>))
+                    : (a.g <= 2 ? launch_decode_paged<64, 2> : (a.g <= 4 ? launch_decode_paged<64, 4> : launch_decode_paged<64, 8>));
+  return f(tmK, tmV, a, s) == cudaSuccess ? SNAPKV_OK : SNAPKV_ERR_CUDA;
 }
