@@ -5,11 +5,13 @@
 // (tiles of 16 rows of d = 128, or 32 of d = 64, through a TMA ring per warp; both products on
 // warp-level matrix instructions with the cache as the 16-row operand; fp32 probabilities in three
 // bf16 terms), the split another: the lengths are known on the device alone and differ, so all tiles
-// of all (sequence, cache head) units are laid end to end and cut into one equal share per block.  A
-// share that covers a unit writes its result; a unit that crosses shares leaves one partial (maximum,
-// sum, unnormalised output) per share, which a second kernel folds in the order of the shares: same
-// bits every run, no counters, nothing to clear.  A warp's ring runs on across units, so that the next
-// unit's tiles are on the way while the present one is merged.
+// of all (sequence, cache head) units are laid end to end and cut into one equal share per WARP.  A
+// unit that lies inside a share is written by its warp, without any barrier: a batch of short
+// sequences is many such units (shares per block, with a merge of its warps behind every unit: 123 us
+// for 64 sequences of 30 to 8000 rows; now NOW_RAGGED).  A unit that crosses shares leaves one partial
+// (maximum, sum, unnormalised output) per share; the block folds those of its own warps once, at its
+// end, and a second kernel those of the blocks, all in the order of the shares: same bits every run,
+// no counters, nothing to clear.  A warp's ring runs on across units.
 // What lies behind a sequence's last row may be anything: scores there are replaced and the values
 // zeroed in registers, in a unit's last tile alone.
 #include <cuda.h>
@@ -47,7 +49,7 @@ struct DecodePagedArgs {
   unsigned long long wait_ns;
   float *out, *lse;
   // workspace: tiles in front of each sequence [B + 1], then [2 * grid] partials of DP_HEADS *
-  // (D + 2) floats: of the unit that a share begins inside, of the one that it begins with
+  // (D + 2) floats: of the unit that a block's shares begin inside, of the last one that they begin
   long long* prefix;
   float* partials;
 };
@@ -58,10 +60,9 @@ __device__ __forceinline__ int rows_of(const DecodePagedArgs& a, int b) {
   return n < 0 ? 0 : (n < most ? n : static_cast<int>(most));
 }
 
-// How many shares the tiles are cut into: one per block, but no fewer tiles than a block has warps.
-__host__ __device__ __forceinline__ int shares(long long total, int grid) {
-  const long long s = (total + DP_WARPS - 1) / DP_WARPS;
-  return s < grid ? static_cast<int>(s) : grid;
+// How many shares the tiles are cut into: one per warp, none of them empty.
+__device__ __forceinline__ int shares(long long total, int grid) {
+  return total < static_cast<long long>(grid) * DP_WARPS ? static_cast<int>(total) : grid * DP_WARPS;
 }
 
 // A walk over the units of a share.
@@ -94,14 +95,20 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   constexpr int HALVES = D / 64;          // 64-element (128-byte) column blocks of a row
   constexpr int KS = D / 16;              // k-steps of S, and pairs of 8-column tiles of the output
   constexpr int BOX = ROWS * 128;         // bytes of one column block of a tile
-  constexpr int PART = DP_HEADS * D;      // floats of a warp's partial output
+  constexpr int PART = DP_HEADS * (D + 2);  // floats of a partial: maxima, sums, outputs
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[DP_WARPS][DP_STAGES];
-  __shared__ float w_m[2][DP_WARPS][DP_HEADS], w_l[2][DP_WARPS][DP_HEADS];
-  __shared__ long long scan_s[DP_WARPS], start_s[2], total_s;
+  __shared__ long long scan_s[DP_WARPS], start_off[DP_WARPS];
+  __shared__ int start_b[DP_WARPS];
+  // a warp's partials: of the unit that its share begins inside, of the last one that it begins
+  struct Left {
+    int b, unit;   // b < 0: none
+    bool more;     // the unit goes on in the next share
+  };
+  __shared__ Left left_s[DP_WARPS][2];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  float* parts = reinterpret_cast<float*>(smem + DP_WARPS * DP_STAGES * DP_STAGE_BYTES);  // [2][warp][head][D]
+  float* parts = reinterpret_cast<float*>(smem + DP_WARPS * DP_STAGES * DP_STAGE_BYTES);  // [warp][2][PART]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int gid = lane >> 2, tig = lane & 3;   // mma fragment coordinates
   const uint32_t ring = smem_u32(smem) + warp * (DP_STAGES * DP_STAGE_BYTES);
@@ -113,11 +120,12 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     for (int s = 0; s < DP_STAGES; ++s) mbar_init(bar + 8u * s, 1);
     mbar_fence_init();
     fence_proxy_async();
+    left_s[warp][0].b = left_s[warp][1].b = start_b[warp] = -1;
   }
   __syncwarp();
   pdl_wait();  // everything above touched this block's shared memory only
 
-  // ---- the block's share.  Every thread adds up the tiles of its run of sequences.
+  // ---- the warps' shares.  Every thread adds up the tiles of its run of sequences.
   const int run = (a.B + DP_THREADS - 1) / DP_THREADS, b_lo = min(static_cast<int>(threadIdx.x) * run, a.B),
             b_hi = min(b_lo + run, a.B);
   long long mine = 0;
@@ -146,37 +154,44 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
   total *= a.units;
   const int S = shares(total, a.grid);
-  if (static_cast<int>(blockIdx.x) >= S) return;
-  const long long lo = static_cast<long long>(blockIdx.x) * total / S, hi = (static_cast<long long>(blockIdx.x) + 1) * total / S;
+  const int share0 = static_cast<int>(blockIdx.x) * DP_WARPS;
+  if (share0 >= S) return;
+  auto bound = [&](int s) { return static_cast<long long>(s < S ? s : S) * total / S; };
   {
     long long p = before * a.units;
     for (int b = b_lo; b < b_hi; ++b) {
       const long long next = p + static_cast<long long>((rows_of(a, b) + ROWS - 1) / ROWS) * a.units;
-      if (p <= lo && lo < next) {
-        start_s[0] = b;
-        start_s[1] = lo - p;
-      }
+      if (next > p && next > bound(share0) && p < bound(share0 + DP_WARPS))
+        for (int w = 0; w < DP_WARPS && share0 + w < S; ++w) {
+          const long long lo = bound(share0 + w);
+          if (p <= lo && lo < next) {
+            start_b[w] = b;
+            start_off[w] = lo - p;
+          }
+        }
       p = next;
     }
   }
   __syncthreads();
-  Walk cur;
-  cur.b = static_cast<int>(start_s[0]);
-  cur.n = rows_of(a, cur.b);
-  cur.tiles = (cur.n + ROWS - 1) / ROWS;
-  cur.unit = static_cast<int>(start_s[1] / cur.tiles);
-  cur.t0 = static_cast<int>(start_s[1] - static_cast<long long>(cur.unit) * cur.tiles);
-  cur.left = hi - lo;
-  cur.t1 = cur.left < cur.tiles - cur.t0 ? cur.t0 + static_cast<int>(cur.left) : cur.tiles;
+  Walk cur = {};
+  if (start_b[warp] >= 0) {
+    cur.b = start_b[warp];
+    cur.n = rows_of(a, cur.b);
+    cur.tiles = (cur.n + ROWS - 1) / ROWS;
+    cur.unit = static_cast<int>(start_off[warp] / cur.tiles);
+    cur.t0 = static_cast<int>(start_off[warp] - static_cast<long long>(cur.unit) * cur.tiles);
+    cur.left = bound(share0 + warp + 1) - bound(share0 + warp);
+    cur.t1 = cur.left < cur.tiles - cur.t0 ? cur.t0 + static_cast<int>(cur.left) : cur.tiles;
+  }
 
-  // ---- the warp's tiles: every DP_WARPS-th of each unit.  `ahead` is the next one to be requested;
-  // its page numbers are fetched when the one before is requested.
+  // ---- the warp's tiles.  `ahead` is at the next one to be requested; its page numbers are fetched
+  // when the one before is requested.
   Walk ahead = cur;
-  int at = cur.t0 + warp, page[ROWS / DP_BOX_ROWS];
+  int at = cur.t0, page[ROWS / DP_BOX_ROWS];
   auto find_page = [&] {  // settles `ahead` on a tile (or behind the share) and fetches its page numbers
-    while (ahead.left > 0 && at >= ahead.t1) {
+    if (ahead.left > 0 && at >= ahead.t1) {
       walk_next<D>(a, ahead);
-      at = ahead.t0 + warp;
+      at = ahead.t0;
     }
     if (ahead.left > 0)
 #pragma unroll
@@ -205,7 +220,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     }
     __syncwarp();
     ++issued;
-    at += DP_WARPS;
+    ++at;
     find_page();
   };
   find_page();
@@ -215,9 +230,9 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const int term0 = (2 * tig) / NH;             // this lane's columns carry terms term0, term0 + 8 / NH, ...
   const int lrow_k = lane & 15, lchunk_k = lane >> 4;
   const int lrow_v = (lane & 7) + ((lane >> 4) << 3), lchunk_v = (lane >> 3) & 1;
-  int n = 0, buf = 0;
+  int n = 0;
   bool failed = false;
-  for (; cur.left > 0; walk_next<D>(a, cur), buf ^= 1) {
+  for (; cur.left > 0; walk_next<D>(a, cur)) {
     const int head = cur.unit / a.chunks, h0 = (cur.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
     // Q as the B operand: column gid is head h0 + gid % NH (zero beyond gc)
     uint32_t qb[KS][2];
@@ -236,7 +251,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of columns 2 tig + {0, 1}; l: this lane's keys
-    for (int t = cur.t0 + warp; t < cur.t1 && !failed; t += DP_WARPS) {
+    for (int t = cur.t0; t < cur.t1 && !failed; ++t) {
       const int s = n % DP_STAGES;
       if (!wait_copy(bar + 8u * s, (n / DP_STAGES) & 1, a.wait_ns)) {
         failed = true;
@@ -332,42 +347,72 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] += __shfl_xor_sync(0xffffffffu, acc[j][i], o);
 
-    // ---- merge the warps, in order (two buffers: a warp may run ahead into the next unit)
-    float* part = parts + buf * (DP_WARPS * PART);
-    if (tig < NH / 2) {
+    if (failed) m[0] = m[1] = 0.f;
+    if (cur.t0 == 0 && cur.t1 == cur.tiles) {  // the whole unit
+      if (tig < NH / 2)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int h = 2 * tig + c;
-        if (gid == 0) {
-          w_m[buf][warp][h] = failed ? 0.f : m[c];
-          w_l[buf][warp][h] = l[c];
-        }
+        for (int c = 0; c < 2; ++c) {
+          const int h = 2 * tig + c;
+          if (h >= gc) continue;
+          const size_t bh = static_cast<size_t>(cur.b) * a.Hq + head * a.g + h0 + h;
+          const float inv = 1.f / l[c];
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          part[(warp * DP_HEADS + h) * D + 16 * j + gid] = acc[j][c];
-          part[(warp * DP_HEADS + h) * D + 16 * j + gid + 8] = acc[j][c + 2];
+          for (int j = 0; j < KS; ++j) {
+            a.out[bh * D + 16 * j + gid] = acc[j][c] * inv;
+            a.out[bh * D + 16 * j + gid + 8] = acc[j][c + 2] * inv;
+          }
+          if (a.lse && gid == 0) a.lse[bh] = (m[c] + log2f(l[c])) * 0.6931471805599453f;
         }
-      }
+    } else {
+      const int which = cur.t0 == 0;
+      float* part = parts + (warp * 2 + which) * PART;
+      if (tig < NH / 2)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int h = 2 * tig + c;
+          if (gid == 0) {
+            part[h] = m[c];
+            part[DP_HEADS + h] = l[c];
+          }
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            part[2 * DP_HEADS + h * D + 16 * j + gid] = acc[j][c];
+            part[2 * DP_HEADS + h * D + 16 * j + gid + 8] = acc[j][c + 2];
+          }
+        }
+      if (lane == 0) left_s[warp][which] = Left{cur.b, cur.unit, cur.t1 < cur.tiles};
     }
-    __syncthreads();
-    const bool complete = cur.t0 == 0 && cur.t1 == cur.tiles;
-    float* slot = a.partials + static_cast<size_t>(2 * blockIdx.x + (cur.t0 == 0)) * (DP_HEADS * (D + 2));
+  }
+
+  // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
+  // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
+  __syncthreads();
+  for (int i = 0; i < 2 * DP_WARPS;) {
+    const Left first = left_s[i >> 1][i & 1];
+    if (first.b < 0) {
+      ++i;
+      continue;
+    }
+    // a unit that begins with warp w goes on as the first entry of warps w + 1, ...
+    int count = 1, w = i >> 1;
+    bool more = first.more;
+    while (more && w + count < DP_WARPS && left_s[w + count][0].b >= 0) more = left_s[w + count++][0].more;
+    const int head = first.unit / a.chunks, h0 = (first.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
+    const bool begun = i & 1, complete = begun && !more;
+    auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
+    float* slot = a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART;
     for (int e = threadIdx.x; e < gc * D; e += DP_THREADS) {
-      const int h = e / D;  // the same in all lanes (D is a multiple of 32): lane w weighs warp w's partial
-      const float wm = w_m[buf][lane % DP_WARPS][h];
-      float M = wm;
-#pragma unroll
-      for (int o = 1; o < DP_WARPS; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = wm == -INFINITY ? 0.f : exp2f(wm - M);
-      const float fl = f * w_l[buf][lane % DP_WARPS][h];
-      float o = 0.f, L = 0.f;
-#pragma unroll
-      for (int w = 0; w < DP_WARPS; ++w) {
-        o += part[w * PART + e] * __shfl_sync(0xffffffffu, f, w);
-        L += __shfl_sync(0xffffffffu, fl, w);
+      const int h = e / D;
+      float M = -INFINITY, L = 0.f, o = 0.f;
+      for (int k = 0; k < count; ++k) M = fmaxf(M, part(k)[h]);
+      for (int k = 0; k < count; ++k) {
+        const float* p = part(k);
+        const float f = p[h] == -INFINITY ? 0.f : exp2f(p[h] - M);
+        L += p[DP_HEADS + h] * f;
+        o += p[2 * DP_HEADS + e] * f;
       }
       if (complete) {
-        const size_t bh = static_cast<size_t>(cur.b) * a.Hq + head * a.g + h0 + h;
+        const size_t bh = static_cast<size_t>(first.b) * a.Hq + head * a.g + h0 + h;
         a.out[bh * D + e % D] = o / L;
         if (a.lse && e % D == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
       } else {
@@ -378,10 +423,11 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         }
       }
     }
+    i = count == 1 ? i + 1 : 2 * (w + count - 1) + 1;
   }
 }
 
-// A block per query head: folds the partials of a unit that crosses shares, in their order.
+// A block per query head: folds the partials of a unit that crosses blocks, in their order.
 template <int D>
 __global__ void __launch_bounds__(D) decode_paged_join_kernel(const DecodePagedArgs a) {
   pdl_wait();
@@ -395,7 +441,8 @@ __global__ void __launch_bounds__(D) decode_paged_join_kernel(const DecodePagedA
     return;
   }
   const int S = shares(total, a.grid);
-  auto owner = [&](long long x) { return static_cast<int>(((x + 1) * S - 1) / total); };  // the largest c: c total / S <= x
+  // the block of the share that holds tile x: the largest c with c total / S <= x, by eights
+  auto owner = [&](long long x) { return static_cast<int>(((x + 1) * S - 1) / total) / DP_WARPS; };
   const long long x0 = p0 * a.units + static_cast<long long>(c * a.chunks + chunk) * tiles;
   const int first = owner(x0), last = owner(x0 + tiles - 1);
   if (first == last) return;  // complete already
@@ -417,7 +464,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <int D, int NH>
 cudaError_t launch_decode_paged(const CUtensorMap& tmK, const CUtensorMap& tmV, const DecodePagedArgs& a, cudaStream_t stream) {
-  constexpr int SMEM = DP_WARPS * DP_STAGES * DP_STAGE_BYTES + 2 * DP_WARPS * DP_HEADS * D * 4 + 1024;
+  constexpr int SMEM = DP_WARPS * DP_STAGES * DP_STAGE_BYTES + 2 * DP_WARPS * DP_HEADS * (D + 2) * 4 + 1024;
   auto kernel = decode_paged_kernel<D, NH>;
   static DeviceOnce ready;
   if (!ready.done()) {
