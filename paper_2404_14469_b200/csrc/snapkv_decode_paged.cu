@@ -7,11 +7,13 @@
 // bf16 terms), the split another: the lengths are known on the device alone and differ, so all tiles
 // of all (sequence, cache head) units are laid end to end and cut into one equal share per WARP.  A
 // unit that lies inside a share is written by its warp, without any barrier: a batch of short
-// sequences is many such units (shares per block, with a merge of its warps behind every unit: 123 us
-// for 64 sequences of 30 to 8000 rows; now NOW_RAGGED).  A unit that crosses shares leaves one partial
-// (maximum, sum, unnormalised output) per share; the block folds those of its own warps once, at its
-// end, and a second kernel those of the blocks, all in the order of the shares: same bits every run,
-// no counters, nothing to clear.  A warp's ring runs on across units.
+// sequences is many such units.  A unit that crosses shares leaves one partial (maximum, sum,
+// unnormalised output) per share; the block folds those of its own warps once, at its end, and the
+// block that has the unit's last share those of the blocks in front of it, in the order of the
+// shares: same bits every run.  It waits (bounded) for a flag beside each partial.  The flags are the
+// call's own 64-bit number, not a count, so that nothing has to be cleared in front of the call; they
+// are taken back by who read them.  A block waits for blocks of lower numbers alone, which wait for
+// nothing before they have published: they need not be resident together.
 // What lies behind a sequence's last row may be anything: scores there are replaced and the values
 // zeroed in registers, in a unit's last tile alone.
 #include <cuda.h>
@@ -19,6 +21,10 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <unistd.h>
+
+#include <atomic>
+#include <chrono>
 
 #include "../../include/snapkv.h"
 #include "decode_mma.cuh"
@@ -35,6 +41,9 @@ constexpr int DP_BOX_ROWS = 16;               // rows per copy: a page holds a w
 constexpr int DP_HEADS = 8;                   // query heads of a unit
 constexpr int DP_THREADS = DP_WARPS * 32;
 constexpr int DP_MAX_GRID = MAX_GRID;
+// What a unit costs a warp beside its tiles (queries to fetch, a result to reduce and write), in tiles:
+// shares are equal in tiles and units.
+constexpr int DP_UNIT_COST = 1;
 
 constexpr int dp_tile_rows(int D) { return DP_STAGE_BYTES / (4 * D); }
 
@@ -48,9 +57,10 @@ struct DecodePagedArgs {
   float c2;
   unsigned long long wait_ns;
   float *out, *lse;
-  // workspace: tiles in front of each sequence [B + 1], then [2 * grid] partials of DP_HEADS *
-  // (D + 2) floats: of the unit that a block's shares begin inside, of the last one that they begin
-  long long* prefix;
+  // workspace: [2 * grid] flags, then as many partials of DP_HEADS * (D + 2) floats: of the unit that
+  // a block's shares begin inside, of the last one that they begin
+  unsigned long long* flags;
+  unsigned long long call;  // what marks a partial of this call as written
   float* partials;
 };
 
@@ -60,23 +70,58 @@ __device__ __forceinline__ int rows_of(const DecodePagedArgs& a, int b) {
   return n < 0 ? 0 : (n < most ? n : static_cast<int>(most));
 }
 
-// How many shares the tiles are cut into: one per warp, none of them empty.
-__device__ __forceinline__ int shares(long long total, int grid) {
-  return total < static_cast<long long>(grid) * DP_WARPS ? static_cast<int>(total) : grid * DP_WARPS;
+__device__ __forceinline__ unsigned long long ld_flag(const unsigned long long* p) {
+  unsigned long long v;
+  asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return v;
 }
+__device__ __forceinline__ void st_flag(unsigned long long* p, unsigned long long v) {
+  asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
+}
+
+// The cut: `total` pieces (a unit's DP_UNIT_COST, then its tiles) in S shares, the first `extra` of
+// them one piece longer.
+struct Cut {
+  long long total, each, extra;
+  int S;
+  __device__ __forceinline__ Cut(long long total_, int most) : total(total_) {
+    S = total < most ? static_cast<int>(total) : most;
+    // (a 64-bit division takes ten times as long)
+    if (S > 0) each = (total >> 32) == 0 ? static_cast<uint32_t>(total) / static_cast<uint32_t>(S) : total / S;
+    else each = 0;
+    extra = total - each * S;
+  }
+  __device__ __forceinline__ long long begin(int s) const { return s * each + (s < extra ? s : extra); }
+  __device__ __forceinline__ int owner(long long x) const {  // the share that holds piece x
+    const long long longer = extra * (each + 1);
+    auto div = [](long long n, long long d) {
+      return ((n | d) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(n) / static_cast<uint32_t>(d)) : n / d;
+    };
+    return static_cast<int>(x < longer ? div(x, each + 1) : extra + div(x - longer, each));
+  }
+};
 
 // A walk over the units of a share.
 struct Walk {
   int b, n, tiles;       // sequence, its rows and tiles per unit
   int unit;              // of the sequence
-  int t0, t1;            // the share's tiles of the unit
-  long long left;        // tiles of the share from t0 on
+  int t0, t1;            // the share's tiles of the unit (none where it has a part of the unit's cost alone)
+  int p1;                // the share's end in pieces of the unit
+  long long left;        // pieces of the share behind p1
+
+  __device__ __forceinline__ void enter(int p0) {  // the unit from piece p0 on; `left` counts from there
+    const int pieces = tiles + DP_UNIT_COST;
+    p1 = left < pieces - p0 ? p0 + static_cast<int>(left) : pieces;
+    left -= p1 - p0;
+    t0 = p0 > DP_UNIT_COST ? p0 - DP_UNIT_COST : 0;
+    t1 = p1 > DP_UNIT_COST ? p1 - DP_UNIT_COST : 0;
+  }
 };
 
+// The next unit of the share; false at its end.
 template <int D>
-__device__ __forceinline__ void walk_next(const DecodePagedArgs& a, Walk& w) {
-  w.left -= w.t1 - w.t0;
-  if (w.left <= 0) return;
+__device__ __forceinline__ bool walk_next(const DecodePagedArgs& a, Walk& w) {
+  if (w.left <= 0) return false;
   if (++w.unit == a.units) {
     w.unit = 0;
     do {
@@ -84,8 +129,8 @@ __device__ __forceinline__ void walk_next(const DecodePagedArgs& a, Walk& w) {
     } while (w.n == 0 && w.b + 1 < a.B);
     w.tiles = (w.n + dp_tile_rows(D) - 1) / dp_tile_rows(D);
   }
-  w.t0 = 0;
-  w.t1 = w.left < w.tiles ? static_cast<int>(w.left) : w.tiles;
+  w.enter(0);
+  return true;
 }
 
 template <int D, int NH>
@@ -106,6 +151,8 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     bool more;     // the unit goes on in the next share
   };
   __shared__ Left left_s[DP_WARPS][2];
+  __shared__ int late_s;
+  __shared__ long long first_tile_s;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   float* parts = reinterpret_cast<float*>(smem + DP_WARPS * DP_STAGES * DP_STAGE_BYTES);  // [warp][2][PART]
@@ -113,7 +160,6 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const int gid = lane >> 2, tig = lane & 3;   // mma fragment coordinates
   const uint32_t ring = smem_u32(smem) + warp * (DP_STAGES * DP_STAGE_BYTES);
   const uint32_t bar = smem_u32(&bars[warp][0]);
-  pdl_launch_dependents();
   if (lane == 0) {
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
@@ -125,11 +171,28 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   __syncwarp();
   pdl_wait();  // everything above touched this block's shared memory only
 
-  // ---- the warps' shares.  Every thread adds up the tiles of its run of sequences.
+  // ---- the warps' shares.  Every thread adds up the pieces of its run of sequences.
+  if (threadIdx.x < 2) a.flags[2 * blockIdx.x + threadIdx.x] = 0;  // (what a wait that gave up may have left)
+  if (threadIdx.x == 0) late_s = 0;
   const int run = (a.B + DP_THREADS - 1) / DP_THREADS, b_lo = min(static_cast<int>(threadIdx.x) * run, a.B),
             b_hi = min(b_lo + run, a.B);
+  auto pieces_of = [&](int b) {  // of one unit
+    const int t = (rows_of(a, b) + ROWS - 1) / ROWS;
+    return static_cast<long long>(t > 0 ? t + DP_UNIT_COST : 0);
+  };
   long long mine = 0;
-  for (int b = b_lo; b < b_hi; ++b) mine += (rows_of(a, b) + ROWS - 1) / ROWS;
+  for (int k = 0; k < run; ++k) {
+    const int b = b_lo + k;
+    const long long p = b < b_hi ? pieces_of(b) : 1;
+    mine += b < b_hi ? p : 0;
+    // sequences without rows: zeros, each by a warp of one block
+    for (unsigned none = __ballot_sync(0xffffffffu, p == 0 && b % gridDim.x == blockIdx.x); none; none &= none - 1) {
+      const size_t bh = static_cast<size_t>(__shfl_sync(0xffffffffu, b, __ffs(none) - 1)) * a.Hq;
+      for (int e = lane; e < a.Hq * D; e += 32) a.out[bh * D + e] = 0.f;
+      if (a.lse)
+        for (int h = lane; h < a.Hq; h += 32) a.lse[bh + h] = -INFINITY;
+    }
+  }
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -138,32 +201,23 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
   if (lane == 31) scan_s[warp] = upto;
   __syncthreads();
-  long long before = upto - mine;
-  long long total = 0;
+  long long before = upto - mine, total = 0;
   for (int w = 0; w < DP_WARPS; ++w) {
     if (w < warp) before += scan_s[w];
     total += scan_s[w];
   }
-  if (blockIdx.x == 0) {  // for the second kernel
-    long long p = before;
-    for (int b = b_lo; b < b_hi; ++b) {
-      a.prefix[b] = p;
-      p += (rows_of(a, b) + ROWS - 1) / ROWS;
-    }
-    if (threadIdx.x == 0) a.prefix[a.B] = total;
-  }
-  total *= a.units;
-  const int S = shares(total, a.grid);
+  const Cut cut(total * a.units, a.grid * DP_WARPS);
   const int share0 = static_cast<int>(blockIdx.x) * DP_WARPS;
-  if (share0 >= S) return;
-  auto bound = [&](int s) { return static_cast<long long>(s < S ? s : S) * total / S; };
+  if (share0 >= cut.S) return;
+  const int shares = min(DP_WARPS, cut.S - share0);
   {
+    const long long from = cut.begin(share0), to = cut.begin(share0 + shares);
     long long p = before * a.units;
-    for (int b = b_lo; b < b_hi; ++b) {
-      const long long next = p + static_cast<long long>((rows_of(a, b) + ROWS - 1) / ROWS) * a.units;
-      if (next > p && next > bound(share0) && p < bound(share0 + DP_WARPS))
-        for (int w = 0; w < DP_WARPS && share0 + w < S; ++w) {
-          const long long lo = bound(share0 + w);
+    for (int b = b_lo; b < b_hi && p < to; ++b) {
+      const long long next = p + pieces_of(b) * a.units;
+      if (next > from)
+        for (int w = 0; w < shares; ++w) {
+          const long long lo = cut.begin(share0 + w);
           if (p <= lo && lo < next) {
             start_b[w] = b;
             start_off[w] = lo - p;
@@ -174,26 +228,35 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
   __syncthreads();
   Walk cur = {};
-  if (start_b[warp] >= 0) {
+  bool some = start_b[warp] >= 0;
+  if (some) {
     cur.b = start_b[warp];
     cur.n = rows_of(a, cur.b);
     cur.tiles = (cur.n + ROWS - 1) / ROWS;
-    cur.unit = static_cast<int>(start_off[warp] / cur.tiles);
-    cur.t0 = static_cast<int>(start_off[warp] - static_cast<long long>(cur.unit) * cur.tiles);
-    cur.left = bound(share0 + warp + 1) - bound(share0 + warp);
-    cur.t1 = cur.left < cur.tiles - cur.t0 ? cur.t0 + static_cast<int>(cur.left) : cur.tiles;
+    const int pieces = cur.tiles + DP_UNIT_COST;
+    cur.unit = static_cast<int>(start_off[warp] / pieces);
+    cur.left = cut.begin(share0 + warp + 1) - cut.begin(share0 + warp);
+    cur.enter(static_cast<int>(start_off[warp] - static_cast<long long>(cur.unit) * pieces));
   }
+  if (threadIdx.x == 0)  // the first tile of the unit that the block begins inside, among all pieces
+    first_tile_s = cut.begin(share0) - (start_off[0] - static_cast<long long>(cur.unit) * (cur.tiles + DP_UNIT_COST)) + DP_UNIT_COST;
 
   // ---- the warp's tiles.  `ahead` is at the next one to be requested; its page numbers are fetched
   // when the one before is requested.
   Walk ahead = cur;
+  bool tiles_left = some;
   int at = cur.t0, page[ROWS / DP_BOX_ROWS];
   auto find_page = [&] {  // settles `ahead` on a tile (or behind the share) and fetches its page numbers
-    if (ahead.left > 0 && at >= ahead.t1) {
-      walk_next<D>(a, ahead);
+    while (tiles_left && at >= ahead.t1) {
+      tiles_left = walk_next<D>(a, ahead);
       at = ahead.t0;
+      // the unit's queries, on their way into L1
+      const int head = ahead.unit / a.chunks, h0 = (ahead.unit - head * a.chunks) * DP_HEADS;
+      const int bytes = min(DP_HEADS, a.g - h0) * D * 2;
+      const char* q = reinterpret_cast<const char*>(a.q + (static_cast<size_t>(ahead.b) * a.Hq + head * a.g + h0) * D);
+      for (int i = lane * 64; i < bytes; i += 32 * 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + i));
     }
-    if (ahead.left > 0)
+    if (tiles_left)
 #pragma unroll
       for (int i = 0; i < ROWS / DP_BOX_ROWS; ++i) {
         const int r = at * ROWS + i * DP_BOX_ROWS;
@@ -203,7 +266,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   };
   int issued = 0;
   auto request = [&] {  // K and V of the tile at hand, then on to the next
-    if (ahead.left <= 0) return;
+    if (!tiles_left) return;
     if (lane == 0) {
       const uint32_t dst = ring + (issued % DP_STAGES) * DP_STAGE_BYTES, bs = bar + 8u * (issued % DP_STAGES);
       const int head = ahead.unit / a.chunks;
@@ -232,7 +295,8 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const int lrow_v = (lane & 7) + ((lane >> 4) << 3), lchunk_v = (lane >> 3) & 1;
   int n = 0;
   bool failed = false;
-  for (; cur.left > 0; walk_next<D>(a, cur)) {
+  for (; some; some = walk_next<D>(a, cur)) {
+    if (cur.t1 <= cur.t0) continue;
     const int head = cur.unit / a.chunks, h0 = (cur.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
     // Q as the B operand: column gid is head h0 + gid % NH (zero beyond gc)
     uint32_t qb[KS][2];
@@ -387,6 +451,8 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
   // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
   __syncthreads();
+  float* own = reinterpret_cast<float*>(smem);  // the rings are idle: this block's part of a unit that ends here
+  Left ending = {-1, 0, false};
   for (int i = 0; i < 2 * DP_WARPS;) {
     const Left first = left_s[i >> 1][i & 1];
     if (first.b < 0) {
@@ -394,13 +460,15 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       continue;
     }
     // a unit that begins with warp w goes on as the first entry of warps w + 1, ...
-    int count = 1, w = i >> 1;
+    const int w = i >> 1;
+    int count = 1;
     bool more = first.more;
     while (more && w + count < DP_WARPS && left_s[w + count][0].b >= 0) more = left_s[w + count++][0].more;
     const int head = first.unit / a.chunks, h0 = (first.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
     const bool begun = i & 1, complete = begun && !more;
+    if (!begun && !more) ending = first;
     auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
-    float* slot = a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART;
+    float* to = !begun && !more ? own : a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART;
     for (int e = threadIdx.x; e < gc * D; e += DP_THREADS) {
       const int h = e / D;
       float M = -INFINITY, L = 0.f, o = 0.f;
@@ -416,48 +484,94 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         a.out[bh * D + e % D] = o / L;
         if (a.lse && e % D == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
       } else {
-        slot[2 * DP_HEADS + e] = o;
+        to[2 * DP_HEADS + e] = o;
         if (e % D == 0) {
-          slot[h] = M;
-          slot[DP_HEADS + h] = L;
+          to[h] = M;
+          to[DP_HEADS + h] = L;
         }
+      }
+    }
+    if (more) {  // the unit ends in a later block
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        __threadfence();
+        st_flag(a.flags + 2 * blockIdx.x + begun, a.call);
       }
     }
     i = count == 1 ? i + 1 : 2 * (w + count - 1) + 1;
   }
+  if (ending.b < 0) return;
+
+  // ---- a unit that began in an earlier block ends here: join the partials of the blocks from there on
+  const int first = cut.owner(first_tile_s) / DP_WARPS, count = static_cast<int>(blockIdx.x) - first;
+  auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0); };
+  auto slot = [&](int k) { return a.partials + static_cast<size_t>(slot_of(k)) * PART; };
+  const int head = ending.unit / a.chunks, h0 = (ending.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
+  const int tid = static_cast<int>(threadIdx.x);
+  if (tid < count) {
+    unsigned long long* flag = a.flags + slot_of(tid);
+    const unsigned long long t0 = globaltimer_ns();
+    while (ld_flag(flag) != a.call)
+      if (globaltimer_ns() - t0 > a.wait_ns) {
+        late_s = 1;
+        break;
+      }
+    *flag = 0;
+  }
+  __syncthreads();
+  float* ml = own + PART;  // [count][DP_HEADS][2]: maxima, which become weights, and sums
+  for (int i = tid; i < count * gc; i += DP_THREADS) {
+    const int k = i / gc, h = i - k * gc;
+    ml[2 * (k * DP_HEADS + h)] = __ldcg(slot(k) + h);
+    ml[2 * (k * DP_HEADS + h) + 1] = __ldcg(slot(k) + DP_HEADS + h);
+  }
+  __syncthreads();
+  if (warp < gc) {  // a head per warp
+    float M = own[warp];
+    for (int k = lane; k < count; k += 32) M = fmaxf(M, ml[2 * (k * DP_HEADS + warp)]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    float L = 0.f;
+    for (int k = lane; k < count; k += 32) {
+      float* x = ml + 2 * (k * DP_HEADS + warp);
+      const float f = *x == -INFINITY ? 0.f : exp2f(*x - M);
+      L += x[1] * f;
+      *x = f;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    __syncwarp();
+    if (lane == 0) {
+      const float f = own[warp] == -INFINITY ? 0.f : exp2f(own[warp] - M);
+      L += own[DP_HEADS + warp] * f;
+      if (late_s) L = NAN;
+      own[warp] = f;
+      own[DP_HEADS + warp] = L;
+      if (a.lse) a.lse[static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0 + warp] = (M + log2f(L)) * 0.6931471805599453f;
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < gc * D; e += DP_THREADS) {
+    const int h = e / D;
+    float o = own[2 * DP_HEADS + e] * own[h];
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) o += __ldcg(slot(k) + 2 * DP_HEADS + e) * ml[2 * (k * DP_HEADS + h)];
+    a.out[(static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0) * D + e] = o / own[DP_HEADS + h];
+  }
 }
 
-// A block per query head: folds the partials of a unit that crosses blocks, in their order.
-template <int D>
-__global__ void __launch_bounds__(D) decode_paged_join_kernel(const DecodePagedArgs a) {
-  pdl_wait();
-  const int b = blockIdx.x / a.Hq, hq = blockIdx.x - b * a.Hq, e = threadIdx.x;
-  const int c = hq / a.g, hg = hq - c * a.g, chunk = hg / DP_HEADS, h = hg - chunk * DP_HEADS;
-  const long long p0 = a.prefix[b], tiles = a.prefix[b + 1] - p0, total = a.prefix[a.B] * a.units;
-  const size_t bh = blockIdx.x;
-  if (tiles == 0) {  // a sequence without rows
-    a.out[bh * D + e] = 0.f;
-    if (a.lse && e == 0) a.lse[bh] = -INFINITY;
-    return;
-  }
-  const int S = shares(total, a.grid);
-  // the block of the share that holds tile x: the largest c with c total / S <= x, by eights
-  auto owner = [&](long long x) { return static_cast<int>(((x + 1) * S - 1) / total) / DP_WARPS; };
-  const long long x0 = p0 * a.units + static_cast<long long>(c * a.chunks + chunk) * tiles;
-  const int first = owner(x0), last = owner(x0 + tiles - 1);
-  if (first == last) return;  // complete already
-  auto slot = [&](int s) { return a.partials + static_cast<size_t>(2 * s + (s == first)) * (DP_HEADS * (D + 2)); };
-  float M = -INFINITY, L = 0.f, o = 0.f;
-  for (int s = first; s <= last; ++s) M = fmaxf(M, __ldcg(slot(s) + h));
-#pragma unroll 4
-  for (int s = first; s <= last; ++s) {
-    const float* p = slot(s);
-    const float f = exp2f(__ldcg(p + h) - M);
-    L += __ldcg(p + DP_HEADS + h) * f;
-    o += __ldcg(p + 2 * DP_HEADS + h * D + e) * f;
-  }
-  a.out[bh * D + e] = o / L;
-  if (a.lse && e == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
+// A number that no other call has: partials of an earlier call, of another process in the same memory
+// or of whatever was there do not pass for this call's.
+unsigned long long call_number() {
+  static const unsigned long long seed =
+      static_cast<unsigned long long>(std::chrono::system_clock::now().time_since_epoch().count()) ^
+      (static_cast<unsigned long long>(getpid()) << 40);
+  static std::atomic<unsigned long long> calls{0};
+  unsigned long long x = seed + ++calls * 0x9e3779b97f4a7c15ull;  // (odd: a step through all 64-bit numbers)
+  x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;                    // mixed one to one
+  x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+  x ^= x >> 31;
+  return x ? x : 1;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -472,9 +586,7 @@ cudaError_t launch_decode_paged(const CUtensorMap& tmK, const CUtensorMap& tmV, 
     if (e != cudaSuccess) return e;
     ready.set();
   }
-  const cudaError_t e = launch_pdl(kernel, dim3(a.grid), dim3(DP_THREADS), SMEM, stream, tmK, tmV, a);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(decode_paged_join_kernel<D>, dim3(a.B * a.Hq), dim3(D), 0, stream, a);
+  return launch_pdl(kernel, dim3(a.grid), dim3(DP_THREADS), SMEM, stream, tmK, tmV, a);
 }
 
 bool strides_ok(const int64_t* s, int d) {
@@ -498,7 +610,7 @@ bool pool_map(CUtensorMap* m, const void* pool, const int64_t* s, int d, int pag
 extern "C" size_t snapkv_decode_paged_workspace_size(int B, int Hq, int Hc, int d) {
   using namespace snapkv;
   if (B < 1 || Hq < 1 || Hc < 1 || Hq % Hc != 0 || (d != 64 && d != 128)) return 0;
-  return align256((static_cast<size_t>(B) + 1) * sizeof(long long)) +
+  return align256(2 * DP_MAX_GRID * sizeof(unsigned long long)) +
          align256(static_cast<size_t>(2) * DP_MAX_GRID * DP_HEADS * (d + 2) * sizeof(float));
 }
 
@@ -539,8 +651,9 @@ extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_
   a.c2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
   a.wait_ns = wait_limit_setting();
   a.out = out, a.lse = out_lse;
-  a.prefix = static_cast<long long*>(workspace);
-  a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256((static_cast<size_t>(B) + 1) * sizeof(long long)));
+  a.flags = static_cast<unsigned long long*>(workspace);
+  a.call = call_number();
+  a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(2 * DP_MAX_GRID * sizeof(unsigned long long)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto f = d == 128 ? (a.g <= 2 ? launch_decode_paged<128, 2> : (a.g <= 4 ? launch_decode_paged<128, 4> : launch_decode_paged<128, 8>))
                     : (a.g <= 2 ? launch_decode_paged<64, 2> : (a.g <= 4 ? launch_decode_paged<64, 4> : launch_decode_paged<64, 8>));
