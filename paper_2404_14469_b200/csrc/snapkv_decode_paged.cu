@@ -79,6 +79,11 @@ __device__ __forceinline__ void st_flag(unsigned long long* p, unsigned long lon
   asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
 }
 
+// (a 64-bit division takes several times as long as one of 32 bits)
+__device__ __forceinline__ long long quotient64(long long n, long long d) {
+  return ((n | d) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(n) / static_cast<uint32_t>(d)) : n / d;
+}
+
 // The cut: `total` pieces (a unit's DP_UNIT_COST, then its tiles) in S shares, the first `extra` of
 // them one piece longer.
 struct Cut {
@@ -86,18 +91,13 @@ struct Cut {
   int S;
   __device__ __forceinline__ Cut(long long total_, int most) : total(total_) {
     S = total < most ? static_cast<int>(total) : most;
-    // (a 64-bit division takes ten times as long)
-    if (S > 0) each = (total >> 32) == 0 ? static_cast<uint32_t>(total) / static_cast<uint32_t>(S) : total / S;
-    else each = 0;
+    each = S > 0 ? quotient64(total, S) : 0;
     extra = total - each * S;
   }
   __device__ __forceinline__ long long begin(int s) const { return s * each + (s < extra ? s : extra); }
   __device__ __forceinline__ int owner(long long x) const {  // the share that holds piece x
     const long long longer = extra * (each + 1);
-    auto div = [](long long n, long long d) {
-      return ((n | d) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(n) / static_cast<uint32_t>(d)) : n / d;
-    };
-    return static_cast<int>(x < longer ? div(x, each + 1) : extra + div(x - longer, each));
+    return static_cast<int>(x < longer ? quotient64(x, each + 1) : extra + quotient64(x - longer, each));
   }
 };
 
@@ -143,14 +143,14 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   constexpr int PART = DP_HEADS * (D + 2);  // floats of a partial: maxima, sums, outputs
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[DP_WARPS][DP_STAGES];
-  __shared__ long long scan_s[DP_WARPS], start_off[DP_WARPS];
-  __shared__ int start_b[DP_WARPS];
+  __shared__ long long scan_s[DP_WARPS], run_s[DP_THREADS];
   // a warp's partials: of the unit that its share begins inside, of the last one that it begins
   struct Left {
     int b, unit;   // b < 0: none
     bool more;     // the unit goes on in the next share
   };
   __shared__ Left left_s[DP_WARPS][2];
+  __shared__ Left ending_s;
   __shared__ int late_s;
   __shared__ long long first_tile_s;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -166,14 +166,17 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     for (int s = 0; s < DP_STAGES; ++s) mbar_init(bar + 8u * s, 1);
     mbar_fence_init();
     fence_proxy_async();
-    left_s[warp][0].b = left_s[warp][1].b = start_b[warp] = -1;
+    left_s[warp][0].b = left_s[warp][1].b = -1;
   }
   __syncwarp();
   pdl_wait();  // everything above touched this block's shared memory only
 
   // ---- the warps' shares.  Every thread adds up the pieces of its run of sequences.
   if (threadIdx.x < 2) a.flags[2 * blockIdx.x + threadIdx.x] = 0;  // (what a wait that gave up may have left)
-  if (threadIdx.x == 0) late_s = 0;
+  if (threadIdx.x == 0) {
+    late_s = 0;
+    ending_s.b = -1;
+  }
   const int run = (a.B + DP_THREADS - 1) / DP_THREADS, b_lo = min(static_cast<int>(threadIdx.x) * run, a.B),
             b_hi = min(b_lo + run, a.B);
   auto pieces_of = [&](int b) {  // of one unit
@@ -199,47 +202,51 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     const long long x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
+  run_s[threadIdx.x] = upto - mine;
   if (lane == 31) scan_s[warp] = upto;
   __syncthreads();
-  long long before = upto - mine, total = 0;
-  for (int w = 0; w < DP_WARPS; ++w) {
-    if (w < warp) before += scan_s[w];
-    total += scan_s[w];
-  }
-  const Cut cut(total * a.units, a.grid * DP_WARPS);
+  long long warp_before[DP_WARPS + 1];  // pieces in front of each warp's runs
+  warp_before[0] = 0;
+#pragma unroll
+  for (int w = 0; w < DP_WARPS; ++w) warp_before[w + 1] = warp_before[w] + scan_s[w];
+  const Cut cut(warp_before[DP_WARPS] * a.units, a.grid * DP_WARPS);
   const int share0 = static_cast<int>(blockIdx.x) * DP_WARPS;
   if (share0 >= cut.S) return;
-  const int shares = min(DP_WARPS, cut.S - share0);
-  {
-    const long long from = cut.begin(share0), to = cut.begin(share0 + shares);
-    long long p = before * a.units;
-    for (int b = b_lo; b < b_hi && p < to; ++b) {
-      const long long next = p + pieces_of(b) * a.units;
-      if (next > from)
-        for (int w = 0; w < shares; ++w) {
-          const long long lo = cut.begin(share0 + w);
-          if (p <= lo && lo < next) {
-            start_b[w] = b;
-            start_off[w] = lo - p;
-          }
-        }
-      p = next;
-    }
-  }
-  __syncthreads();
   Walk cur = {};
-  bool some = start_b[warp] >= 0;
+  bool some = share0 + warp < cut.S;
+  long long off = 0;  // of the warp's share in its first sequence, then in its first unit
   if (some) {
-    cur.b = start_b[warp];
-    cur.n = rows_of(a, cur.b);
+    // the run that holds the share's first piece: the last one that begins at or in front of it
+    const long long lo = cut.begin(share0 + warp);
+    int in = 0;
+    long long from = 0;
+#pragma unroll
+    for (int w = 0; w < DP_WARPS; ++w) {
+      const long long p = (warp_before[w] + run_s[w * 32 + lane]) * a.units;
+      const unsigned reached = __ballot_sync(0xffffffffu, p <= lo);
+      if (reached) {
+        const int last = 31 - __clz(reached);
+        in = w * 32 + last;
+        from = __shfl_sync(0xffffffffu, p, last);
+      }
+    }
+    cur.b = in * run;
+    off = lo - from;
+    for (;; ++cur.b) {  // its sequences
+      cur.n = rows_of(a, cur.b);
+      const long long size = pieces_of(cur.b) * a.units;
+      if (off < size || cur.b + 1 >= a.B) break;
+      off -= size;
+    }
     cur.tiles = (cur.n + ROWS - 1) / ROWS;
     const int pieces = cur.tiles + DP_UNIT_COST;
-    cur.unit = static_cast<int>(start_off[warp] / pieces);
-    cur.left = cut.begin(share0 + warp + 1) - cut.begin(share0 + warp);
-    cur.enter(static_cast<int>(start_off[warp] - static_cast<long long>(cur.unit) * pieces));
+    cur.unit = static_cast<int>(quotient64(off, pieces));
+    off -= static_cast<long long>(cur.unit) * pieces;
+    cur.left = cut.begin(share0 + warp + 1) - lo;
+    cur.enter(static_cast<int>(off));
   }
   if (threadIdx.x == 0)  // the first tile of the unit that the block begins inside, among all pieces
-    first_tile_s = cut.begin(share0) - (start_off[0] - static_cast<long long>(cur.unit) * (cur.tiles + DP_UNIT_COST)) + DP_UNIT_COST;
+    first_tile_s = cut.begin(share0) - off + DP_UNIT_COST;
 
   // ---- the warp's tiles.  `ahead` is at the next one to be requested; its page numbers are fetched
   // when the one before is requested.
@@ -450,56 +457,76 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 
   // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
   // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
+  // The warp with which a unit begins folds it, the last warp what the block begins inside.
   __syncthreads();
   float* own = reinterpret_cast<float*>(smem);  // the rings are idle: this block's part of a unit that ends here
-  Left ending = {-1, 0, false};
-  for (int i = 0; i < 2 * DP_WARPS;) {
-    const Left first = left_s[i >> 1][i & 1];
-    if (first.b < 0) {
-      ++i;
-      continue;
-    }
-    // a unit that begins with warp w goes on as the first entry of warps w + 1, ...
+  auto fold = [&](int i) {
+    const Left begin = left_s[i >> 1][i & 1];
+    if (begin.b < 0) return;
     const int w = i >> 1;
     int count = 1;
-    bool more = first.more;
+    bool more = begin.more;
     while (more && w + count < DP_WARPS && left_s[w + count][0].b >= 0) more = left_s[w + count++][0].more;
-    const int head = first.unit / a.chunks, h0 = (first.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
+    const int head = begin.unit / a.chunks, h0 = (begin.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
     const bool begun = i & 1, complete = begun && !more;
-    if (!begun && !more) ending = first;
+    const size_t bh = static_cast<size_t>(begin.b) * a.Hq + head * a.g + h0;
     auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
-    float* to = !begun && !more ? own : a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART;
-    for (int e = threadIdx.x; e < gc * D; e += DP_THREADS) {
-      const int h = e / D;
-      float M = -INFINITY, L = 0.f, o = 0.f;
-      for (int k = 0; k < count; ++k) M = fmaxf(M, part(k)[h]);
-      for (int k = 0; k < count; ++k) {
-        const float* p = part(k);
-        const float f = p[h] == -INFINITY ? 0.f : exp2f(p[h] - M);
-        L += p[DP_HEADS + h] * f;
-        o += p[2 * DP_HEADS + e] * f;
-      }
-      if (complete) {
-        const size_t bh = static_cast<size_t>(first.b) * a.Hq + head * a.g + h0 + h;
-        a.out[bh * D + e % D] = o / L;
-        if (a.lse && e % D == 0) a.lse[bh] = (M + log2f(L)) * 0.6931471805599453f;
-      } else {
-        to[2 * DP_HEADS + e] = o;
-        if (e % D == 0) {
-          to[h] = M;
-          to[DP_HEADS + h] = L;
+    float* to = complete ? nullptr : (begun || more ? a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART : own);
+    constexpr int E = D / 32;  // elements of a head per lane
+    for (int q = 0; q < gc; q += 4) {
+      // four heads of eight partials, a lane each: maxima, weights, sums
+      const int k = lane & 7, hl = q + (lane >> 3);
+      const bool in = k < count && hl < gc;
+      const float mk = in ? part(k)[hl] : -INFINITY;
+      float M = mk;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      const float f = mk == -INFINITY ? 0.f : exp2f(mk - M);
+      float L = in ? part(k)[DP_HEADS + hl] * f : 0.f;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+#pragma unroll
+      for (int hq = 0; hq < 4; ++hq) {
+        const int h = q + hq;
+        const float Lh = __shfl_sync(0xffffffffu, L, 8 * hq), Mh = __shfl_sync(0xffffffffu, M, 8 * hq);
+        float o[E] = {};
+#pragma unroll
+        for (int k = 0; k < DP_WARPS; ++k) {
+          const float fk = __shfl_sync(0xffffffffu, f, 8 * hq + k);
+          if (h < gc && k < count) {
+            const float* p = part(k) + 2 * DP_HEADS + h * D + E * lane;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(p[e], fk, o[e]);
+          }
+        }
+        if (h >= gc) continue;
+        if (complete) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) a.out[(bh + h) * D + E * lane + e] = o[e] / Lh;
+          if (a.lse && lane == 0) a.lse[bh + h] = (Mh + log2f(Lh)) * 0.6931471805599453f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) to[2 * DP_HEADS + h * D + E * lane + e] = o[e];
+          if (lane == 0) {
+            to[h] = Mh;
+            to[DP_HEADS + h] = Lh;
+          }
         }
       }
     }
     if (more) {  // the unit ends in a later block
-      __syncthreads();
-      if (threadIdx.x == 0) {
+      __syncwarp();
+      if (lane == 0) {
         __threadfence();
         st_flag(a.flags + 2 * blockIdx.x + begun, a.call);
       }
     }
-    i = count == 1 ? i + 1 : 2 * (w + count - 1) + 1;
-  }
+    if (!begun && !more && lane == 0) ending_s = begin;
+  };
+  fold(2 * warp + 1);
+  if (warp == DP_WARPS - 1) fold(0);
+  __syncthreads();
+  const Left ending = ending_s;
   if (ending.b < 0) return;
 
   // ---- a unit that began in an earlier block ends here: join the partials of the blocks from there on
