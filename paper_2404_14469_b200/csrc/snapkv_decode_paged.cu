@@ -151,7 +151,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   };
   __shared__ Left left_s[DP_WARPS][2];
   __shared__ Left ending_s;
-  __shared__ int late_s;
+  __shared__ int late_s, publish_s[2];
   __shared__ long long first_tile_s;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -174,7 +174,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   // ---- the warps' shares.  Every thread adds up the pieces of its run of sequences.
   if (threadIdx.x < 2) a.flags[2 * blockIdx.x + threadIdx.x] = 0;  // (what a wait that gave up may have left)
   if (threadIdx.x == 0) {
-    late_s = 0;
+    late_s = publish_s[0] = publish_s[1] = 0;
     ending_s.b = -1;
   }
   const int run = (a.B + DP_THREADS - 1) / DP_THREADS, b_lo = min(static_cast<int>(threadIdx.x) * run, a.B),
@@ -212,6 +212,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const Cut cut(warp_before[DP_WARPS] * a.units, a.grid * DP_WARPS);
   const int share0 = static_cast<int>(blockIdx.x) * DP_WARPS;
   if (share0 >= cut.S) return;
+  const int shares = min(DP_WARPS, cut.S - share0);  // of the block
   Walk cur = {};
   bool some = share0 + warp < cut.S;
   long long off = 0;  // of the warp's share in its first sequence, then in its first unit
@@ -457,86 +458,83 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 
   // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
   // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
-  // The warp with which a unit begins folds it, the last warp what the block begins inside.
+  // A warp folds a head of a unit.  From here on the code runs once, so it is bound by fetching
+  // instructions: rolled loops (unrolled ones took 2.5 us for the fold and 3 for the join instead of
+  // NOW_FOLD).
   __syncthreads();
   float* own = reinterpret_cast<float*>(smem);  // the rings are idle: this block's part of a unit that ends here
-  auto fold = [&](int i) {
-    const Left begin = left_s[i >> 1][i & 1];
-    if (begin.b < 0) return;
-    const int w = i >> 1;
+  constexpr int E = D / 32;  // elements of a head per lane
+  uint32_t present, more;
+  {
+    const Left x = lane < 2 * DP_WARPS ? left_s[lane >> 1][lane & 1] : Left{-1, 0, false};
+    present = __ballot_sync(0xffffffffu, x.b >= 0);
+    more = __ballot_sync(0xffffffffu, x.b >= 0 && x.more);
+  }
+  constexpr uint32_t EVEN = 0x55555555u & ((1u << 2 * DP_WARPS) - 1);
+  int item = 0;
+  for (uint32_t begins = present & ~(EVEN & ~1u); begins; begins &= begins - 1) {
+    const int i = __ffs(begins) - 1, w = i >> 1;
+    const Left u = left_s[w][i & 1];
     int count = 1;
-    bool more = begin.more;
-    while (more && w + count < DP_WARPS && left_s[w + count][0].b >= 0) more = left_s[w + count++][0].more;
-    const int head = begin.unit / a.chunks, h0 = (begin.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
-    const bool begun = i & 1, complete = begun && !more;
-    const size_t bh = static_cast<size_t>(begin.b) * a.Hq + head * a.g + h0;
-    auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
-    float* to = complete ? nullptr : (begun || more ? a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART : own);
-    constexpr int E = D / 32;  // elements of a head per lane
-    for (int q = 0; q < gc; q += 4) {
-      // four heads of eight partials, a lane each: maxima, weights, sums
-      const int k = lane & 7, hl = q + (lane >> 3);
-      const bool in = k < count && hl < gc;
-      const float mk = in ? part(k)[hl] : -INFINITY;
-      float M = mk;
+    bool on = more >> i & 1;  // the unit goes on: to the first later entry of a share that it does not fill, if there is one
+    if (on) {
+      const uint32_t ends = present & ~more & EVEN & ~((2u << i) - 1);
+      on = ends == 0;
+      count = (on ? shares : (__ffs(ends) + 1) / 2) - w;
+    }
+    const int head = u.unit / a.chunks, h0 = (u.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
+    const bool begun = i & 1, complete = begun && !on;
+    float* to = begun || on ? a.partials + static_cast<size_t>(2 * blockIdx.x + begun) * PART : own;
+#pragma unroll 1
+    for (int h = 0; h < gc; ++h) {
+      if (item++ % DP_WARPS != warp) continue;
+      auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
+      const int mine = lane & 7;
+      const float mk = mine < count ? part(mine)[h] : -INFINITY;
+      float M = fmaxf(mk, -1e30f), L = 0.f, o[E] = {};
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = mk == -INFINITY ? 0.f : exp2f(mk - M);
-      float L = in ? part(k)[DP_HEADS + hl] * f : 0.f;
+      for (int x = 1; x < 8; x <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+      const float f = ex2_approx(mk - M);
+#pragma unroll 1
+      for (int k = 0; k < count; ++k) {
+        const float fk = __shfl_sync(0xffffffffu, f, k);
+        const float* p = part(k);
+        L = fmaf(p[DP_HEADS + h], fk, L);
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+        for (int e = 0; e < E; ++e) o[e] = fmaf(p[2 * DP_HEADS + h * D + E * lane + e], fk, o[e]);
+      }
+      if (complete) {
+        const size_t bh = static_cast<size_t>(u.b) * a.Hq + head * a.g + h0 + h;
+        const float inv = __fdividef(1.f, L);
 #pragma unroll
-      for (int hq = 0; hq < 4; ++hq) {
-        const int h = q + hq;
-        const float Lh = __shfl_sync(0xffffffffu, L, 8 * hq), Mh = __shfl_sync(0xffffffffu, M, 8 * hq);
-        float o[E] = {};
+        for (int e = 0; e < E; ++e) a.out[bh * D + E * lane + e] = o[e] * inv;
+        if (a.lse && lane == 0) a.lse[bh] = (M + __log2f(L)) * 0.6931471805599453f;
+      } else {
 #pragma unroll
-        for (int k = 0; k < DP_WARPS; ++k) {
-          const float fk = __shfl_sync(0xffffffffu, f, 8 * hq + k);
-          if (h < gc && k < count) {
-            const float* p = part(k) + 2 * DP_HEADS + h * D + E * lane;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(p[e], fk, o[e]);
-          }
-        }
-        if (h >= gc) continue;
-        if (complete) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) a.out[(bh + h) * D + E * lane + e] = o[e] / Lh;
-          if (a.lse && lane == 0) a.lse[bh + h] = (Mh + log2f(Lh)) * 0.6931471805599453f;
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) to[2 * DP_HEADS + h * D + E * lane + e] = o[e];
-          if (lane == 0) {
-            to[h] = Mh;
-            to[DP_HEADS + h] = Lh;
-          }
+        for (int e = 0; e < E; ++e) to[2 * DP_HEADS + h * D + E * lane + e] = o[e];
+        if (lane == 0) {
+          to[h] = M;
+          to[DP_HEADS + h] = L;
+          if (h == 0 && on) publish_s[begun] = 1;  // the unit ends in a later block
+          if (h == 0 && !on) ending_s = u;
         }
       }
     }
-    if (more) {  // the unit ends in a later block
-      __syncwarp();
-      if (lane == 0) {
-        __threadfence();
-        st_flag(a.flags + 2 * blockIdx.x + begun, a.call);
-      }
-    }
-    if (!begun && !more && lane == 0) ending_s = begin;
-  };
-  fold(2 * warp + 1);
-  if (warp == DP_WARPS - 1) fold(0);
+  }
   __syncthreads();
+  if (threadIdx.x < 2 && publish_s[threadIdx.x]) {
+    __threadfence();
+    st_flag(a.flags + 2 * blockIdx.x + threadIdx.x, a.call);
+  }
   const Left ending = ending_s;
   if (ending.b < 0) return;
 
   // ---- a unit that began in an earlier block ends here: join the partials of the blocks from there on
   const int first = cut.owner(first_tile_s) / DP_WARPS, count = static_cast<int>(blockIdx.x) - first;
   auto slot_of = [&](int k) { return 2 * (first + k) + (k == 0); };
-  auto slot = [&](int k) { return a.partials + static_cast<size_t>(slot_of(k)) * PART; };
   const int head = ending.unit / a.chunks, h0 = (ending.unit - head * a.chunks) * DP_HEADS, gc = min(DP_HEADS, a.g - h0);
-  const int tid = static_cast<int>(threadIdx.x);
-  if (tid < count) {
-    unsigned long long* flag = a.flags + slot_of(tid);
+  if (static_cast<int>(threadIdx.x) < count) {
+    unsigned long long* flag = a.flags + slot_of(threadIdx.x);
     const unsigned long long t0 = globaltimer_ns();
     while (ld_flag(flag) != a.call)
       if (globaltimer_ns() - t0 > a.wait_ns) {
@@ -546,45 +544,52 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     *flag = 0;
   }
   __syncthreads();
-  float* ml = own + PART;  // [count][DP_HEADS][2]: maxima, which become weights, and sums
-  for (int i = tid; i < count * gc; i += DP_THREADS) {
-    const int k = i / gc, h = i - k * gc;
-    ml[2 * (k * DP_HEADS + h)] = __ldcg(slot(k) + h);
-    ml[2 * (k * DP_HEADS + h) + 1] = __ldcg(slot(k) + DP_HEADS + h);
-  }
-  __syncthreads();
-  if (warp < gc) {  // a head per warp
-    float M = own[warp];
-    for (int k = lane; k < count; k += 32) M = fmaxf(M, ml[2 * (k * DP_HEADS + warp)]);
+  // DP_WARPS / 2^x warps per head, each with every so many-th partial; then theirs and the block's own
+  const int heads_log2 = gc > 4 ? 3 : (gc > 2 ? 2 : (gc > 1 ? 1 : 0)), ways = DP_WARPS >> heads_log2;
+  const int h = warp & ((1 << heads_log2) - 1), way = warp >> heads_log2;
+  float* sums = own + PART + warp * (D + 2);  // [warp]: maximum, sum, output
+  float M = -1e30f, L = 0.f, o[E] = {};
+  if (h < gc) {
+#pragma unroll 4
+    for (int k = way; k < count; k += ways) {
+      const float* p = a.partials + static_cast<size_t>(slot_of(k)) * PART;
+      const float mk = __ldcg(p + h), lk = __ldcg(p + DP_HEADS + h);
+      float x[E];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float L = 0.f;
-    for (int k = lane; k < count; k += 32) {
-      float* x = ml + 2 * (k * DP_HEADS + warp);
-      const float f = *x == -INFINITY ? 0.f : exp2f(*x - M);
-      L += x[1] * f;
-      *x = f;
+      for (int e = 0; e < E; ++e) x[e] = __ldcg(p + 2 * DP_HEADS + h * D + E * lane + e);
+      const float Mn = fmaxf(M, mk), c = ex2_approx(M - Mn), f = ex2_approx(mk - Mn);
+      M = Mn;
+      L = fmaf(L, c, lk * f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, x[e] * f);
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    __syncwarp();
     if (lane == 0) {
-      const float f = own[warp] == -INFINITY ? 0.f : exp2f(own[warp] - M);
-      L += own[DP_HEADS + warp] * f;
-      if (late_s) L = NAN;
-      own[warp] = f;
-      own[DP_HEADS + warp] = L;
-      if (a.lse) a.lse[static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0 + warp] = (M + log2f(L)) * 0.6931471805599453f;
+      sums[0] = M;
+      sums[1] = L;
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[2 + E * lane + e] = o[e];
   }
   __syncthreads();
-  for (int e = tid; e < gc * D; e += DP_THREADS) {
-    const int h = e / D;
-    float o = own[2 * DP_HEADS + e] * own[h];
-#pragma unroll 8
-    for (int k = 0; k < count; ++k) o += __ldcg(slot(k) + 2 * DP_HEADS + e) * ml[2 * (k * DP_HEADS + h)];
-    a.out[(static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0) * D + e] = o / own[DP_HEADS + h];
+  if (way > 0 || h >= gc) return;
+#pragma unroll 1
+  for (int k = 1; k <= ways; ++k) {
+    const bool last = k == ways;
+    const float* p = last ? own : sums + (k << heads_log2) * (D + 2);
+    const float mk = last ? own[h] : p[0], lk = last ? own[DP_HEADS + h] : p[1];
+    const float* x = last ? own + 2 * DP_HEADS + h * D : p + 2;
+    const float Mn = fmaxf(M, mk), c = ex2_approx(M - Mn), f = ex2_approx(mk - Mn);
+    M = Mn;
+    L = fmaf(L, c, lk * f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, x[E * lane + e] * f);
   }
+  if (late_s) L = NAN;
+  const size_t bh = static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0 + h;
+  const float inv = __fdividef(1.f, L);
+#pragma unroll
+  for (int e = 0; e < E; ++e) a.out[bh * D + E * lane + e] = o[e] * inv;
+  if (a.lse && lane == 0) a.lse[bh] = (M + __log2f(L)) * 0.6931471805599453f;
 }
 
 // A number that no other call has: partials of an earlier call, of another process in the same memory
