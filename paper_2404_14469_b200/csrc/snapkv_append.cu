@@ -1,5 +1,10 @@
 // Appending to a paged cache with the position rotation on the way.  Pair r of a head turns by
 // positions[t] * inv_freq[r]: (x, y) -> (x cos - y sin, x sin + y cos).
+//
+// Bound by HBM for prompts, by latency for a generation step.  A block takes a few tokens with all
+// their heads.  First a warp per token finds the token's sequence, page and angles, once for all heads;
+// then a thread moves items of 16 elements (two 16-byte vectors: the two halves of eight pairs) of one
+// token and one place in the head, head after head, so that its sines and cosines stay in registers.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -24,77 +29,151 @@ struct AppendArgs {
   long long kp[3], vp[3];
 };
 
-// The sequence of token t, its place in it and whether there is one.
-__device__ __forceinline__ bool locate(const AppendArgs& a, int t, int* b, int* i) {
-  if (!a.cu) {
-    const int n = a.T / a.B;
-    *b = t / n;
-    *i = t - *b * n;
-    return true;
+// The last sequence that starts at or in front of token t, and its start: a warp probes 32 at a time.
+__device__ __forceinline__ int sequence_of(const AppendArgs& a, int t, int lane, int* start) {
+  int lo = 0, len = a.B;
+  for (;;) {
+    const int step = (len + 31) / 32;
+    const int v = lane * step < len ? __ldg(a.cu + lo + lane * step) : 0x7fffffff;
+    const int last = 31 - __clz(__ballot_sync(0xffffffffu, v <= t) | 1u);
+    lo += last * step;
+    if (step == 1) {
+      *start = __shfl_sync(0xffffffffu, v, last);
+      return lo;
+    }
+    len = min(step, len - last * step);
   }
-  if (t >= a.cu[a.B] || t < a.cu[0]) return false;
-  int lo = 0, hi = a.B - 1;  // the last sequence that starts at or in front of t
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.cu[mid] <= t) lo = mid;
-    else hi = mid - 1;
+}
+
+__device__ __forceinline__ float lo_bf16(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// TB tokens per block: 8 where there are many (a head's rows are then consecutive in memory for eight
+// tokens in caches stored by heads), 1 for generation steps.
+template <int D, bool INTERLEAVED, int TB>
+__global__ void __launch_bounds__(AP_THREADS) append_kernel(const AppendArgs a) {
+  constexpr int ITEMS = D / 16;                        // of a head
+  constexpr int STEP = AP_THREADS / (ITEMS * TB);      // heads in flight
+  __shared__ float cs[TB][D / 2], sn[TB][D / 2];
+  __shared__ long long src_b[TB], src_i[TB], k_to[TB], v_to[TB];  // sequence and row of the source; targets or -1
+  __shared__ int live[TB];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  if (warp < TB) {
+    const int t = blockIdx.x * TB + warp;
+    int b = 0, start = 0;
+    bool in = t < a.T;
+    if (in && a.cu) {
+      in = t < __ldg(a.cu + a.B);
+      b = sequence_of(a, t, lane, &start);
+      in = in && t >= start;
+    } else if (in) {
+      const int n = a.T / a.B;
+      b = t / n;
+      start = b * n;
+    }
+    if (in) {
+      const long long slot = static_cast<long long>(__ldg(a.cache_lens + b)) + (t - start);
+      const long long pos = a.positions ? __ldg(a.positions + t) : slot;
+      // Angles of far positions lose their fraction of a turn in 32 bits: 64 up to the reduction.
+      for (int r = lane; r < a.half; r += 32) {
+        const double turns = static_cast<double>(pos) * __ldg(a.inv_freq + r) * 0.15915494309189535;  // 1 / (2 pi)
+        sincospif(2.f * static_cast<float>(turns - rint(turns)), &sn[warp][r], &cs[warp][r]);
+      }
+      if (lane == 0) {
+        src_b[warp] = a.cu ? 0 : b;
+        src_i[warp] = a.cu ? t : t - start;
+        long long kd = -1, vd = -1;
+        if (slot >= 0 && slot < static_cast<long long>(a.pages_per_seq) * a.page_size) {
+          const int s = static_cast<int>(slot), pg = s / a.page_size, row = s - pg * a.page_size;
+          const int page = __ldg(a.table + static_cast<long long>(b) * a.pages_per_seq + pg);
+          if (page >= 0 && page < a.num_pages) {
+            kd = page * a.kp[0] + row * a.kp[2];
+            vd = page * a.vp[0] + row * a.vp[2];
+          }
+        }
+        k_to[warp] = kd;
+        v_to[warp] = vd;
+      }
+    }
+    if (lane == 0) live[warp] = in;
   }
-  *b = lo;
-  *i = t - a.cu[lo];
-  return true;
+  __syncthreads();
+  const int j = threadIdx.x % ITEMS, tok = threadIdx.x / ITEMS % TB, h0 = threadIdx.x / (ITEMS * TB);
+  if (!live[tok]) return;
+  // the item's two vectors, and whether it is turned
+  const bool turn = 8 * j < a.half;
+  const int v0 = turn && !INTERLEAVED ? j : 2 * j, v1 = turn && !INTERLEAVED ? j + a.half / 8 : 2 * j + 1;
+  float c[8], s[8];
+  if (turn)
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(&cs[tok][8 * j + e]), y = *reinterpret_cast<const float4*>(&sn[tok][8 * j + e]);
+      c[e] = x.x, c[e + 1] = x.y, c[e + 2] = x.z, c[e + 3] = x.w;
+      s[e] = y.x, s[e + 1] = y.y, s[e + 2] = y.z, s[e + 3] = y.w;
+    }
+  auto turned = [&](uint4& p, uint4& q) {
+    uint32_t x[4] = {p.x, p.y, p.z, p.w}, y[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (INTERLEAVED) {  // pairs (lo, hi): of the first vector 0 .. 3, of the second 4 .. 7
+        const float xl = lo_bf16(x[i]), xh = hi_bf16(x[i]), yl = lo_bf16(y[i]), yh = hi_bf16(y[i]);
+        x[i] = pack_bf16(xl * c[i] - xh * s[i], xl * s[i] + xh * c[i]);
+        y[i] = pack_bf16(yl * c[4 + i] - yh * s[4 + i], yl * s[4 + i] + yh * c[4 + i]);
+      } else {
+        const float xl = lo_bf16(x[i]), xh = hi_bf16(x[i]), yl = lo_bf16(y[i]), yh = hi_bf16(y[i]);
+        x[i] = pack_bf16(xl * c[2 * i] - yl * s[2 * i], xh * c[2 * i + 1] - yh * s[2 * i + 1]);
+        y[i] = pack_bf16(xl * s[2 * i] + yl * c[2 * i], xh * s[2 * i + 1] + yh * c[2 * i + 1]);
+      }
+    }
+    p = make_uint4(x[0], x[1], x[2], x[3]);
+    q = make_uint4(y[0], y[1], y[2], y[3]);
+  };
+  // heads h0, h0 + STEP, ... of a tensor, four at a time in flight
+  auto move = [&](const uint16_t* from, long long from_head, int heads, bool rotate, uint16_t* to, long long to_head, int reps) {
+    for (int h = h0; h < heads; h += 4 * STEP) {
+      uint4 x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (h + i * STEP < heads) {
+          const uint4* p = reinterpret_cast<const uint4*>(from + (h + i * STEP) * from_head);
+          x[i] = p[v0];
+          y[i] = p[v1];
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (h + i * STEP < heads) {
+          if (rotate) turned(x[i], y[i]);
+          uint16_t* base = to + (h + i * STEP) * reps * to_head;
+          for (int m = 0; m < reps; ++m) {
+            uint4* p = reinterpret_cast<uint4*>(base + m * to_head);
+            p[v0] = x[i];
+            p[v1] = y[i];
+          }
+        }
+    }
+  };
+  const long long b = src_b[tok], i = src_i[tok], kd = k_to[tok], vd = v_to[tok];
+  const int reps = a.Hc / a.Hkv;
+  if (kd >= 0) {
+    move(a.k + b * a.k_st[0] + i * a.k_st[1], a.k_st[2], a.Hkv, turn, a.k_pool + kd, a.kp[1], reps);
+    move(a.v + b * a.v_st[0] + i * a.v_st[1], a.v_st[2], a.Hkv, false, a.v_pool + vd, a.vp[1], reps);
+  }
+  if (a.q)
+    move(a.q + b * a.q_st[0] + i * a.q_st[1], a.q_st[2], a.Hq, turn,
+         a.q_out + (static_cast<long long>(blockIdx.x) * TB + tok) * a.Hq * D, D, 1);
 }
 
 template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(AP_THREADS) append_kernel(const AppendArgs a) {
-  __shared__ float cs[D / 2], sn[D / 2];
-  pdl_wait();
-  const int t = blockIdx.x;
-  int b, i;
-  if (!locate(a, t, &b, &i)) return;
-  const long long slot = static_cast<long long>(a.cache_lens[b]) + i;
-  // Angles of far positions lose their fraction of a turn in 32 bits: 64 up to the reduction.
-  for (int r = threadIdx.x; r < a.half; r += AP_THREADS) {
-    const double angle = static_cast<double>(a.positions ? a.positions[t] : slot) * a.inv_freq[r];
-    const double turns = angle * 0.15915494309189535;  // 1 / (2 pi)
-    sincospif(2.f * static_cast<float>(turns - rint(turns)), &sn[r], &cs[r]);
-  }
-  __syncthreads();
-  uint16_t *kd = nullptr, *vd = nullptr;
-  if (slot >= 0 && slot < static_cast<long long>(a.pages_per_seq) * a.page_size) {
-    const int pg = static_cast<int>(slot / a.page_size), row = static_cast<int>(slot - static_cast<long long>(pg) * a.page_size);
-    const int page = a.table[static_cast<long long>(b) * a.pages_per_seq + pg];
-    if (page >= 0 && page < a.num_pages) {
-      kd = a.k_pool + page * a.kp[0] + row * a.kp[2];
-      vd = a.v_pool + page * a.vp[0] + row * a.vp[2];
-    }
-  }
-  const long long at = a.cu ? t : i, seq = a.cu ? 0 : b;
-  const uint16_t* ks = a.k + seq * a.k_st[0] + at * a.k_st[1];
-  const uint16_t* vs = a.v + seq * a.v_st[0] + at * a.v_st[1];
-  const uint16_t* qs = a.q ? a.q + seq * a.q_st[0] + at * a.q_st[1] : nullptr;
-  auto turned = [&](const uint16_t* x, int c) {  // element c of a rotated head
-    const float self = __uint_as_float(static_cast<uint32_t>(x[c]) << 16);
-    if (c >= 2 * a.half) return x[c];
-    const int r = INTERLEAVED ? c >> 1 : (c < a.half ? c : c - a.half);
-    const bool first = INTERLEAVED ? !(c & 1) : c < a.half;
-    const int oc = INTERLEAVED ? c ^ 1 : (first ? c + a.half : c - a.half);
-    const float other = __uint_as_float(static_cast<uint32_t>(x[oc]) << 16);
-    const __nv_bfloat16 y = __float2bfloat16(first ? self * cs[r] - other * sn[r] : other * sn[r] + self * cs[r]);
-    return __bfloat16_as_ushort(y);
-  };
-  const int reps = a.Hc / a.Hkv;
-  if (kd)
-    for (int e = threadIdx.x; e < a.Hkv * D; e += AP_THREADS) {
-      const int h = e / D, c = e % D;
-      const uint16_t x = turned(ks + h * a.k_st[2], c), y = vs[h * a.v_st[2] + c];
-      for (int m = 0; m < reps; ++m) {
-        kd[(h * reps + m) * a.kp[1] + c] = x;
-        vd[(h * reps + m) * a.vp[1] + c] = y;
-      }
-    }
-  if (qs)
-    for (int e = threadIdx.x; e < a.Hq * D; e += AP_THREADS)
-      a.q_out[static_cast<long long>(t) * a.Hq * D + e] = turned(qs + e / D * a.q_st[2], e % D);
+cudaError_t launch_append(const AppendArgs& a, cudaStream_t stream) {
+  // eight tokens per block once that leaves every SM a few blocks
+  if (a.T >= 8 * 4 * sm_count())
+    return launch_pdl(append_kernel<D, INTERLEAVED, 8>, dim3((a.T + 7) / 8), dim3(AP_THREADS), 0, stream, a);
+  return launch_pdl(append_kernel<D, INTERLEAVED, 1>, dim3(a.T), dim3(AP_THREADS), 0, stream, a);
 }
 
 bool token_strides_ok(const int64_t* s, int d) {
@@ -160,8 +239,7 @@ extern "C" snapkv_status_t snapkv_append_paged(const void* k_new, const void* v_
   a.q_out = static_cast<uint16_t*>(q_out);
   a.k_pool = static_cast<uint16_t*>(k_pool);
   a.v_pool = static_cast<uint16_t*>(v_pool);
-  auto kernel = d == 128 ? (interleaved ? append_kernel<128, true> : append_kernel<128, false>)
-                         : (interleaved ? append_kernel<64, true> : append_kernel<64, false>);
-  const cudaError_t e = launch_pdl(kernel, dim3(T), dim3(AP_THREADS), 0, static_cast<cudaStream_t>(stream), a);
-  return e == cudaSuccess ? SNAPKV_OK : SNAPKV_ERR_CUDA;
+  auto f = d == 128 ? (interleaved ? launch_append<128, true> : launch_append<128, false>)
+                    : (interleaved ? launch_append<64, true> : launch_append<64, false>);
+  return f(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SNAPKV_OK : SNAPKV_ERR_CUDA;
 }

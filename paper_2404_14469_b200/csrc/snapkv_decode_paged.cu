@@ -42,8 +42,9 @@ constexpr int DP_HEADS = 8;                   // query heads of a unit
 constexpr int DP_THREADS = DP_WARPS * 32;
 constexpr int DP_MAX_GRID = MAX_GRID;
 // What a unit costs a warp beside its tiles (queries to fetch, a result to reduce and write), in tiles:
-// shares are equal in tiles and units.
-constexpr int DP_UNIT_COST = 1;
+// shares are equal in tiles and units.  (64 sequences of 20 to 300 rows: 14.9 us with 1, 14.0 with 2,
+// 13.8 with 3; of 30 to 8000 rows 62.7, 61.9, 62.1.)
+constexpr int DP_UNIT_COST = 2;
 
 constexpr int dp_tile_rows(int D) { return DP_STAGE_BYTES / (4 * D); }
 
@@ -459,8 +460,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
   // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
   // A warp folds a head of a unit.  From here on the code runs once, so it is bound by fetching
-  // instructions: rolled loops (unrolled ones took 2.5 us for the fold and 3 for the join instead of
-  // NOW_FOLD).
+  // instructions: rolled loops (for one sequence of 777 rows the call takes 9.5 us, 13.2 with unrolled ones).
   __syncthreads();
   float* own = reinterpret_cast<float*>(smem);  // the rings are idle: this block's part of a unit that ends here
   constexpr int E = D / 32;  // elements of a head per lane

@@ -217,6 +217,39 @@ def test_append_with_rotation(d, rot, interleaved, Hq, Hkv, Hc, page):
     assert ((got.double() - ref).abs() <= plain64.rotate_tolerance(ref, size)).all()
 
 
+@pytest.mark.parametrize("d,rot,interleaved,Hq,Hkv,Hc,counts", [
+    (128, 128, False, 6, 2, 6, [5000, 1, 0, 777]),      # many tokens: several share a block
+    (64, 32, True, 3, 1, 1, [13, 6001]),
+    (128, 96, True, 4, 4, 4, [2, 3] * 1100),            # more sequences than one probe of a warp tells apart
+    (64, 64, False, 2, 2, 2, [1] * 40 + [0] * 5 + [7]),
+    (128, 64, False, 33, 3, 33, [1, 2]),                # more heads than a block takes at a time
+])
+def test_append_many_tokens_and_sequences(d, rot, interleaved, Hq, Hkv, Hc, counts):
+    page = 16
+    before = [3 * b % 20 for b in range(len(counts))]
+    k_pool, v_pool, table = _cache([x + n for x, n in zip(before, counts)], Hc, page, d, rot)
+    g = _gen(rot + Hq)
+    T = sum(counts)
+    f = _bf16(g, T, Hq + 2 * Hkv, d)
+    q, k, v = f[:, :Hq], f[:, Hq:Hq + Hkv], f[:, Hq + Hkv:]
+    pos = torch.randint(0, 400000, (T,), generator=g, device="cuda", dtype=torch.int32)
+    starts = torch.cumsum(torch.tensor([0] + counts), 0)
+    b = torch.repeat_interleave(torch.arange(len(counts)), torch.tensor(counts))
+    slot = torch.tensor(before)[b] + torch.arange(T) - starts[b]
+    where = (table.long()[b.cuda(), (slot // page).cuda()], slice(None), (slot % page).cuda())
+    kr, size = plain64.rotate(k, pos, FREQ(rot), interleaved)
+    rep = lambda x: x.repeat_interleave(Hc // Hkv, 1)
+    want_k, want_v, tol = k_pool.double(), v_pool.clone(), torch.zeros_like(k_pool, dtype=torch.float64)
+    want_k[where], want_v[where], tol[where] = rep(kr), rep(v), rep(plain64.rotate_tolerance(kr, size))
+    got = sk.snapkv_append_paged(k, v, k_pool, v_pool, table, _i32(before), starts.to(torch.int32).cuda(), pos, FREQ(rot),
+                                 interleaved, q)
+    assert torch.equal(torch.nan_to_num(v_pool, 1e30), torch.nan_to_num(want_v, 1e30))
+    err = (torch.nan_to_num(k_pool.double(), 1e30) - torch.nan_to_num(want_k, 1e30)).abs()
+    assert (err <= tol).all()
+    ref, size = plain64.rotate(q, pos, FREQ(rot), interleaved)
+    assert ((got.double() - ref).abs() <= plain64.rotate_tolerance(ref, size)).all()
+
+
 @pytest.mark.parametrize("Hc,n", [(2, 1), (2, 50), (8, 33)])
 def test_append_dense_batches_at_their_cache_rows(Hc, n):
     B, Hq, Hkv, d, page, before = 3, 8, 2, 128, 64, [0, 100, 63]
