@@ -7,13 +7,15 @@
 // largest power of two that divides the group is packed into a tile, (token, head) with the head
 // fastest: 32 tokens of 4 heads instead of 128 of one, so that a unit's two tiles need the same keys
 // but for a few.  Both products run on tcgen05 over 128 keys at a time:
-//   S = Q.K^T into TMEM; a warpgroup per tile reads it back, a query row per thread (maximum and sum
-//   need no shuffles), and writes P = exp2(S c - m) in bf16 over it; O += P.V with P as the operand in
-//   TMEM and O in TMEM to the end.
+//   S = Q.K^T into TMEM; two warpgroups per tile read it back, half of a query row's keys per thread
+//   (no shuffles; the halves exchange their maxima through shared memory), and write P = exp2(S c - m)
+//   in bf16 over it; O += P.V with P as the operand in TMEM and O in TMEM to the end.
 // The reference m of a row moves only when the maximum has risen by more than 2^8 (or at the row's
 // first tile): then the thread rescales its row of O, which is still for as long as P is not handed
 // over.  P <= 2^8 loses nothing in bf16, and the rows of most tiles move nothing.
-// Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  Persistent: a block's next unit has its
+// A tile's chain - S, softmax, P.V, and no S before that as P lies over it - is what bounds the kernel:
+// with one warpgroup per tile a scheduler had a single warp of it to issue from.
+// Warps: 0-7 softmax of tile 0, 8-15 of tile 1, 16 TMA, 17 MMA.  Persistent: a block's next unit has its
 // keys on the way while the present one is written out.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -30,7 +32,7 @@ namespace snapkv {
 namespace {
 
 constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
-constexpr int PF_THREADS = 320;
+constexpr int PF_THREADS = 576;
 constexpr int PF_KEYS = 128;      // keys per tile
 constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
 
@@ -61,10 +63,14 @@ struct PfSmem {
   static constexpr int TILE = COLS * PF_BLOCK;          // one tile of Q, K or V
   static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
   static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
-  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile s_full, p_full, pv_done, o_free, and drain
-  static constexpr int NBAR = 2 * STAGES + 2 + 8 + 1;
+  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile s_full, p_full, pv_done, o_free, drain, and
+  // one for each pair of warps that share rows
+  static constexpr int NBAR = 2 * STAGES + 2 + 8 + 1 + 8;
   static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
-  static constexpr int DYN_BYTES = OFF_MISC + 16 + 1024;
+  static constexpr int OFF_XCH = OFF_MISC + 16;           // float [2 tiles][2 halves][128 rows]
+  // Room for a start at a multiple of 1024 bytes: the kernel has no static shared memory, and its
+  // dynamic one starts at a multiple of 256 at least.
+  static constexpr int DYN_BYTES = OFF_XCH + 2048 + 768;
   static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
 };
 
@@ -100,7 +106,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   using SM = PfSmem<D>;
   constexpr int COLS = SM::COLS, STAGES = SM::STAGES, TILE = SM::TILE;
   constexpr int TMEM_O = 256;   // S (and P over it) of tile t at 128 t, O at TMEM_O + D t
-  extern __shared__ uint8_t smem_raw[];
+  extern __shared__ __align__(256) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   const uint32_t sbase = smem_u32(smem);
@@ -113,6 +119,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   auto bar_pv = [&](int t) { return bar_qe + 8u * (5 + t); };
   auto bar_of = [&](int t) { return bar_qe + 8u * (7 + t); };
   const uint32_t bar_drain = bar_qe + 8u * 9;
+  auto bar_pair = [&](int i) { return bar_qe + 8u * (10 + i); };
   volatile uint32_t* tmem_ptr_s = reinterpret_cast<volatile uint32_t*>(smem + SM::OFF_MISC);
   volatile int* abort_s = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -127,16 +134,17 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     mbar_init(bar_qe, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(bar_s(t), 1);
-      mbar_init(bar_p(t), 4);
+      mbar_init(bar_p(t), 8);
       mbar_init(bar_pv(t), 1);
-      mbar_init(bar_of(t), 4);
+      mbar_init(bar_of(t), 8);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(bar_pair(i), 2);
     mbar_init(bar_drain, 1);
     *abort_s = 0;
     *reinterpret_cast<volatile unsigned long long*>(abort_s + 1) = a.wait_ns;
     mbar_fence_init();
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_s)), 512);
     tmem_relinquish();
   }
@@ -174,7 +182,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   };
   Unit u;
 
-  if (warp == 8) {
+  if (warp == 16) {
     // ------------------------------------------------------------ TMA
     if (elect_one()) {
       int fill = 0, nq = 0;
@@ -206,7 +214,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == 17) {
     // ------------------------------------------------------------ MMA
     if (elect_one()) {
       constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16(128, D) | UMMA_B_MN_MAJOR;
@@ -266,11 +274,25 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         drain(bar_drain, 0, a.wait_ns);
       }
     }
-  } else {
+  } else if (warp < 16) {
     // ------------------------------------------------------------ softmax
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + TMEM_O + D * t;
+    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + TMEM_O + D * t + D / 2 * half;
+    const uint32_t bar_x = bar_pair(t * 4 + quarter);
+    // The threads with the two halves of a row meet here.
+    int nx = 0;
+    auto meet = [&] {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_x);
+      if (!mbar_wait_warp(bar_x, nx++ & 1, abort_s, 10)) return false;
+      tc_fence_after();
+      return true;
+    };
+    // a maximum (or sum) per thread; [half][row] of the tile
+    float* mine_s = reinterpret_cast<float*>(smem + SM::OFF_XCH) + t * 256 + 128 * half + row;
+    const float* other_s = reinterpret_cast<float*>(smem + SM::OFF_XCH) + t * 256 + 128 * (half ^ 1) + row;
     const unsigned long long scale2 = pack2(a.c2, a.c2);
     int ns = 0, npv = 0;
     bool ok = true;
@@ -278,47 +300,51 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
-      const int jmax = u.n0 + min(token, u.lq - 1);             // the last key that the row sees
-      const int jfree = u.n0 + u.token0 + t * tile_tokens;      // every row of the tile sees keys up to here
-      float m = -INFINITY, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m)
+      const int jmax = u.n0 + min(token, u.lq - 1) - 64 * half;   // the last key that the row sees, from this half's first on
+      const int jfree = u.n0 + u.token0 + t * tile_tokens;        // every row of the tile sees keys up to here
+      float m = -INFINITY, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m) over this half's keys
       for (int j = 0; ok && j < nk; ++j) {
         ok = mbar_wait_warp(bar_s(t), ns++ & 1, abort_s, 8);
         if (!ok) break;
         tc_fence_after();
-        float v[4][32];
+        float v[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, v[c]);
+        for (int c = 0; c < 2; ++c) tmem_ld32(s_at + 64 * half + 32 * c, v[c]);
         tmem_wait_ld();
         if (j * PF_KEYS + PF_KEYS - 1 > jfree) {
           const int see = jmax - j * PF_KEYS;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[c][i] = 32 * c + i <= see ? v[c][i] : -INFINITY;
         }
         float mx[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          mx[c] = fmaxf(v[c][0], v[c][1]);
+          mx[c] = v[c >> 1][(c & 1) * 16];
 #pragma unroll
-          for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(mx[c], fmaxf(v[c][i], v[c][i + 1]));
+          for (int i = 1; i < 15; i += 2) mx[c] = fmaxf(fmaxf(mx[c], v[c >> 1][(c & 1) * 16 + i]), v[c >> 1][(c & 1) * 16 + i + 1]);
+          mx[c] = fmaxf(mx[c], v[c >> 1][(c & 1) * 16 + 15]);
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c2;
+        float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        *mine_s = top;  // (the other thread has read the last one: it had handed over its P then)
+        // from here on the other half's scores are in registers, too: P may be written over them
+        ok = meet();
+        if (!ok) break;
+        top = fmaxf(top, *other_s) * a.c2;
         // (a row that sees no key keeps minus infinity, with 0 as its reference in the differences)
         const bool move = top > m + 8.f;
         if (j > 0 && __any_sync(0xffffffffu, move)) {
           const float f = move ? ex2_approx(m - top) : 1.f;  // O is still: its last product was through before S
           l *= f;
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            float o[32];
-            tmem_ld32(o_at + 32 * c, o);
+          for (int c = 0; c < D / 2; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_at + c, o);
             tmem_wait_ld();
-            uint32_t w[2][16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) w[i >> 4][i & 15] = __float_as_uint(o[i] * f);
-            tmem_st16(o_at + 32 * c, w[0]);
-            tmem_st16(o_at + 32 * c + 16, w[1]);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(o_at + c, o);
           }
         }
         if (j == 0 || move) m = top;
@@ -326,7 +352,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         const unsigned long long negm = pack2(neg, neg);
         unsigned long long sum = 0ull;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
           uint32_t w[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
@@ -337,7 +363,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
             const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
             w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h);
           }
-          tmem_st16(s_at + 16 * c, w);
+          tmem_st16(s_at + 32 * half + 16 * c, w);
         }
         const float2 both = unpack2(sum);
         l += both.x + both.y;
@@ -349,34 +375,36 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       }
       // ---- the tile's result
       if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (npv - 1) & 1, abort_s, 9);
+      if (ok && nk > 0) {
+        *mine_s = l;
+        ok = meet();
+        if (ok) l = half ? *other_s + l : l + *other_s;
+        ok = ok && meet();  // (both have read)
+      }
       tc_fence_after();
-      const float inv = ok ? (l > 0.f ? 1.f / l : 0.f) : NAN;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
       const bool mine = token < u.lq;
       const long long at = (u.q0 + token) * a.Hq + head;
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        float o[32];
+      for (int c = 0; c < D / 2; c += 16) {
+        uint32_t o[16] = {};
         if (ok && nk > 0) {
-          tmem_ld32(o_at + 32 * c, o);
+          tmem_ld16(o_at + c, o);
           tmem_wait_ld();
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0.f;
         }
-        if (mine) {
-          uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + 32 * c);
+        if (!mine) continue;
+        uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + D / 2 * half + c);
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            uint32_t w[4];
+        for (int i = 0; i < 16; i += 8) {
+          uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // (a row without keys may have read what another unit left in O)
-              const float x = l > 0.f || !ok ? o[i + 2 * e] * inv : 0.f, y = l > 0.f || !ok ? o[i + 2 * e + 1] * inv : 0.f;
-              const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-              w[e] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            dst[i >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < 4; ++e) {
+            // (a row without keys has what another unit left in O)
+            const float x = l > 0.f ? __uint_as_float(o[i + 2 * e]) * inv : 0.f, y = l > 0.f ? __uint_as_float(o[i + 2 * e + 1]) * inv : 0.f;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+            w[e] = ok && !isnan(l) ? *reinterpret_cast<const uint32_t*>(&h) : 0x7fff7fffu;
           }
+          dst[i >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
       if (ok && nk > 0) {
@@ -384,8 +412,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_of(t));
       }
-      if (mine) {
-        const float e = ok ? (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY) : NAN;
+      if (mine && half == 0) {
+        const float e = !ok || isnan(l) ? NAN : (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY);
         if (a.lse) a.lse[at] = e;
         const int w = token - (u.lq - a.W);
         if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
@@ -394,7 +422,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 17) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
