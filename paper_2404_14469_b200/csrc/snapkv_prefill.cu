@@ -7,15 +7,15 @@
 // largest power of two that divides the group is packed into a tile, (token, head) with the head
 // fastest: 32 tokens of 4 heads instead of 128 of one, so that a unit's two tiles need the same keys
 // but for a few.  Both products run on tcgen05 over 128 keys at a time:
-//   S = Q.K^T into TMEM; two warpgroups per tile read it back, half of a query row's keys per thread
-//   (no shuffles; the halves exchange their maxima through shared memory), and write P = exp2(S c - m)
-//   in bf16 over it; O += P.V with P as the operand in TMEM and O in TMEM to the end.
-// The reference m of a row moves only when the maximum has risen by more than 2^8 (or at the row's
-// first tile): then the thread rescales its row of O, which is still for as long as P is not handed
-// over.  P <= 2^8 loses nothing in bf16, and the rows of most tiles move nothing.
-// A tile's chain - S, softmax, P.V, and no S before that as P lies over it - is what bounds the kernel:
-// with one warpgroup per tile a scheduler had a single warp of it to issue from.
-// Warps: 0-7 softmax of tile 0, 8-15 of tile 1, 16 TMA, 17 MMA.  Persistent: a block's next unit has its
+//   S = Q.K^T into TMEM; a warpgroup per tile reads it back, a query row per thread (no shuffles), and
+//   writes P = exp2(S c - m) in bf16 over it; O += P.V with P as the operand in TMEM and O in TMEM to
+//   the end.
+// What bounds the kernel is a tile's chain: S, its weights, P.V, and no S before that as P lies over it.
+// So the weights do not wait for a maximum, and none is taken: the reference m of a row is its maximum
+// over the first key tile and moves only when later weights pass 2^64, which shows in their sum.  The
+// row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
+// in two halves, so that the product with V runs while the second one is computed.
+// Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  Persistent: a block's next unit has its
 // keys on the way while the present one is written out.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -32,8 +32,11 @@ namespace snapkv {
 namespace {
 
 constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
-constexpr int PF_THREADS = 576;
+constexpr int PF_THREADS = 320;
 constexpr int PF_KEYS = 128;      // keys per tile
+// A row takes a new reference when 64 of its weights add up to more than 2^64 (PF_FAR).  That loses
+// nothing: weights and their sums are floating-point numbers, far from fp32's and bf16's 2^127.
+constexpr float PF_FAR = 18446744073709551616.f;
 constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
 
 struct PrefillSeq {
@@ -63,14 +66,11 @@ struct PfSmem {
   static constexpr int TILE = COLS * PF_BLOCK;          // one tile of Q, K or V
   static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
   static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
-  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile s_full, p_full, pv_done, o_free, drain, and
-  // one for each pair of warps that share rows
-  static constexpr int NBAR = 2 * STAGES + 2 + 8 + 1 + 8;
+  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile: S, the halves of P, the product with
+  // the first of them, the whole product, O read out; and drain
+  static constexpr int NBAR = 2 * STAGES + 2 + 12 + 1;
   static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
-  static constexpr int OFF_XCH = OFF_MISC + 16;           // float [2 tiles][2 halves][128 rows]
-  // Room for a start at a multiple of 1024 bytes: the kernel has no static shared memory, and its
-  // dynamic one starts at a multiple of 256 at least.
-  static constexpr int DYN_BYTES = OFF_XCH + 2048 + 768;
+  static constexpr int DYN_BYTES = OFF_MISC + 16 + 1024;
   static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
 };
 
@@ -106,7 +106,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   using SM = PfSmem<D>;
   constexpr int COLS = SM::COLS, STAGES = SM::STAGES, TILE = SM::TILE;
   constexpr int TMEM_O = 256;   // S (and P over it) of tile t at 128 t, O at TMEM_O + D t
-  extern __shared__ __align__(256) uint8_t smem_raw[];
+  extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   const uint32_t sbase = smem_u32(smem);
@@ -115,11 +115,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   auto bar_empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
   const uint32_t bar_qf = bar0 + 8u * (2 * STAGES), bar_qe = bar_qf + 8u;
   auto bar_s = [&](int t) { return bar_qe + 8u * (1 + t); };
-  auto bar_p = [&](int t) { return bar_qe + 8u * (3 + t); };
-  auto bar_pv = [&](int t) { return bar_qe + 8u * (5 + t); };
-  auto bar_of = [&](int t) { return bar_qe + 8u * (7 + t); };
-  const uint32_t bar_drain = bar_qe + 8u * 9;
-  auto bar_pair = [&](int i) { return bar_qe + 8u * (10 + i); };
+  auto bar_p = [&](int t, int h) { return bar_qe + 8u * (3 + 2 * t + h); };
+  auto bar_ph = [&](int t) { return bar_qe + 8u * (7 + t); };
+  auto bar_pv = [&](int t) { return bar_qe + 8u * (9 + t); };
+  auto bar_of = [&](int t) { return bar_qe + 8u * (11 + t); };
+  const uint32_t bar_drain = bar_qe + 8u * 13;
   volatile uint32_t* tmem_ptr_s = reinterpret_cast<volatile uint32_t*>(smem + SM::OFF_MISC);
   volatile int* abort_s = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -134,17 +134,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     mbar_init(bar_qe, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(bar_s(t), 1);
-      mbar_init(bar_p(t), 8);
+      mbar_init(bar_p(t, 0), 4);
+      mbar_init(bar_p(t, 1), 4);
+      mbar_init(bar_ph(t), 1);
       mbar_init(bar_pv(t), 1);
-      mbar_init(bar_of(t), 8);
+      mbar_init(bar_of(t), 4);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(bar_pair(i), 2);
     mbar_init(bar_drain, 1);
     *abort_s = 0;
     *reinterpret_cast<volatile unsigned long long*>(abort_s + 1) = a.wait_ns;
     mbar_fence_init();
   }
-  if (warp == 17) {
+  if (warp == 9) {
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_ptr_s)), 512);
     tmem_relinquish();
   }
@@ -182,7 +183,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   };
   Unit u;
 
-  if (warp == 16) {
+  if (warp == 8) {
     // ------------------------------------------------------------ TMA
     if (elect_one()) {
       int fill = 0, nq = 0;
@@ -214,11 +215,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
       }
     }
-  } else if (warp == 17) {
+  } else if (warp == 9) {
     // ------------------------------------------------------------ MMA
     if (elect_one()) {
       constexpr uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16(128, D) | UMMA_B_MN_MAJOR;
-      int use = 0, nq = 0, np[2] = {0, 0}, npv[2] = {0, 0}, no[2] = {0, 0};
+      int use = 0, nq = 0, npv[2] = {0, 0}, no[2] = {0, 0};
       bool ok = true;
       auto full = [&](int i) { return mbar_wait_thread(bar_full(i % STAGES), i / STAGES & 1, abort_s, 3); };
       auto scores = [&](int t, int i) {  // S of tile t with the keys of ring entry i
@@ -235,16 +236,19 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         return true;
       };
       auto values = [&](int t, int i, bool first) {
-        if (!mbar_wait_thread(bar_p(t), np[t]++ & 1, abort_s, 5)) return false;
         // (a unit's first product overwrites O: the unit before must have been read out)
         if (first && !mbar_wait_thread(bar_of(t), (no[t]++ & 1) ^ 1, abort_s, 6)) return false;
         const uint64_t vd = umma_desc_mn128(kv_s + (i % STAGES) * TILE, PF_BLOCK);
-        tc_fence_after();
 #pragma unroll
-        for (int k = 0; k < PF_KEYS / 16; ++k)
-          tc_mma_bf16_ts(tmem + TMEM_O + D * t, tmem + 128 * t + 8 * k, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o,
-                         !first || k != 0);
-        tc_commit(bar_pv(t));
+        for (int h = 0; h < 2; ++h) {
+          if (!mbar_wait_thread(bar_p(t, h), npv[t] & 1, abort_s, 5)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 4 * h; k < 4 * h + 4; ++k)
+            tc_mma_bf16_ts(tmem + TMEM_O + D * t, tmem + 128 * t + 8 * k, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o,
+                           !first || k != 0);
+          tc_commit(h ? bar_pv(t) : bar_ph(t));
+        }
         ++npv[t];
         return true;
       };
@@ -274,126 +278,136 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         drain(bar_drain, 0, a.wait_ns);
       }
     }
-  } else if (warp < 16) {
+  } else {
     // ------------------------------------------------------------ softmax
-    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + TMEM_O + D * t + D / 2 * half;
-    const uint32_t bar_x = bar_pair(t * 4 + quarter);
-    // The threads with the two halves of a row meet here.
-    int nx = 0;
-    auto meet = [&] {
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_x);
-      if (!mbar_wait_warp(bar_x, nx++ & 1, abort_s, 10)) return false;
-      tc_fence_after();
-      return true;
-    };
-    // a maximum (or sum) per thread; [half][row] of the tile
-    float* mine_s = reinterpret_cast<float*>(smem + SM::OFF_XCH) + t * 256 + 128 * half + row;
-    const float* other_s = reinterpret_cast<float*>(smem + SM::OFF_XCH) + t * 256 + 128 * (half ^ 1) + row;
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + TMEM_O + D * t;
     const unsigned long long scale2 = pack2(a.c2, a.c2);
-    int ns = 0, npv = 0;
+    int ns = 0;  // key tiles so far
     bool ok = true;
     for (int r = 0; unit_at(r, &u); ++r) {
       const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
-      const int jmax = u.n0 + min(token, u.lq - 1) - 64 * half;   // the last key that the row sees, from this half's first on
-      const int jfree = u.n0 + u.token0 + t * tile_tokens;        // every row of the tile sees keys up to here
-      float m = -INFINITY, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m) over this half's keys
-      for (int j = 0; ok && j < nk; ++j) {
-        ok = mbar_wait_warp(bar_s(t), ns++ & 1, abort_s, 8);
+      const int jmax = u.n0 + min(token, u.lq - 1);             // the last key that the row sees
+      const int jfree = u.n0 + u.token0 + t * tile_tokens;      // every row of the tile sees keys up to here
+      float m = 0.f, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m)
+      for (int j = 0; ok && j < nk; ++j, ++ns) {
+        ok = mbar_wait_warp(bar_s(t), ns & 1, abort_s, 8);
         if (!ok) break;
         tc_fence_after();
-        float v[2][32];
+        auto mask = [&](float (&x)[32], int c) {
+          if (j * PF_KEYS + PF_KEYS - 1 > jfree) {
+            const int see = jmax - j * PF_KEYS - 32 * c;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) tmem_ld32(s_at + 64 * half + 32 * c, v[c]);
-        tmem_wait_ld();
-        if (j * PF_KEYS + PF_KEYS - 1 > jfree) {
-          const int see = jmax - j * PF_KEYS;
+            for (int i = 0; i < 32; ++i) x[i] = i <= see ? x[i] : -INFINITY;
+          }
+        };
+        auto largest = [&](const float (&x)[32]) {
+          float y = x[0];
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[c][i] = 32 * c + i <= see ? v[c][i] : -INFINITY;
-        }
-        float mx[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx[c] = v[c >> 1][(c & 1) * 16];
-#pragma unroll
-          for (int i = 1; i < 15; i += 2) mx[c] = fmaxf(fmaxf(mx[c], v[c >> 1][(c & 1) * 16 + i]), v[c >> 1][(c & 1) * 16 + i + 1]);
-          mx[c] = fmaxf(mx[c], v[c >> 1][(c & 1) * 16 + 15]);
-        }
-        float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        *mine_s = top;  // (the other thread has read the last one: it had handed over its P then)
-        // from here on the other half's scores are in registers, too: P may be written over them
-        ok = meet();
-        if (!ok) break;
-        top = fmaxf(top, *other_s) * a.c2;
-        // (a row that sees no key keeps minus infinity, with 0 as its reference in the differences)
-        const bool move = top > m + 8.f;
-        if (j > 0 && __any_sync(0xffffffffu, move)) {
-          const float f = move ? ex2_approx(m - top) : 1.f;  // O is still: its last product was through before S
-          l *= f;
+          for (int i = 1; i < 32; ++i) y = fmaxf(y, x[i]);
+          return y;
+        };
+        if (j == 0) {  // the reference: the row's maximum over the first tile
+          float top = -INFINITY;
 #pragma unroll 1
-          for (int c = 0; c < D / 2; c += 16) {
-            uint32_t o[16];
-            tmem_ld16(o_at + c, o);
+          for (int c = 0; c < 4; ++c) {
+            float x[32];
+            tmem_ld32(s_at + 32 * c, x);
             tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st16(o_at + c, o);
+            pin(x);
+            mask(x, c);
+            top = fmaxf(top, largest(x));
           }
+          m = top == -INFINITY ? 0.f : top * a.c2;  // (no key in sight, or none that weighs anything)
         }
-        if (j == 0 || move) m = top;
-        const float neg = m == -INFINITY ? 0.f : -m;
-        const unsigned long long negm = pack2(neg, neg);
-        unsigned long long sum = 0ull;
+        // Half of the keys at a time: their scores are on the way while the first half is worked on.
+        float v[2][32];
+        tmem_ld32(s_at, v[0]);
+        tmem_ld32(s_at + 32, v[1]);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t w[16];
+        for (int h = 0; h < 2; ++h) {
+          tmem_wait_ld();
+          pin(v[0]);
+          pin(v[1]);
+          mask(v[0], 2 * h);
+          mask(v[1], 2 * h + 1);
+          uint32_t w[2][16];
+          float sum[2];
+          auto weights = [&](int c) {
+            const unsigned long long negm = pack2(-m, -m);
+            unsigned long long s2[2] = {0ull, 0ull};
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const unsigned long long p = ex2_approx2(fma2(pack2(v[c][i], v[c][i + 1]), scale2, negm));
-            sum = add2(sum, p);
-            const float2 x = unpack2(p);
-            // to bf16, half a step of 2^-8 of a probability whose fp32 value is in the sum
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
-            w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int i = 0; i < 32; i += 2) {
+              const unsigned long long p = ex2_approx2(fma2(pack2(v[c][i], v[c][i + 1]), scale2, negm));
+              s2[i >> 1 & 1] = add2(s2[i >> 1 & 1], p);
+              const float2 y = unpack2(p);
+              // to bf16, half a step of 2^-8 of a probability whose fp32 value is in the sum
+              const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
+              w[c][i >> 1] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            const float2 y = unpack2(add2(s2[0], s2[1]));
+            sum[c] = y.x + y.y;
+          };
+          weights(0);
+          weights(1);
+          if (__any_sync(0xffffffffu, sum[0] + sum[1] > PF_FAR)) {
+            // A row passed its reference by far: a new one, by a power of two (P rescales exactly).
+            const bool move = sum[0] + sum[1] > PF_FAR;
+            const float top = fmaxf(largest(v[0]), largest(v[1])) * a.c2;
+            const float up = move ? ceilf(top - m) : 0.f, f = ex2_approx(-up);
+            m += up;
+            l *= f;
+            if (h == 1) {  // the first half of P is handed over: its product must be through
+              ok = mbar_wait_warp(bar_ph(t), ns & 1, abort_s, 9);
+              tc_fence_after();
+            }
+            if (j > 0 || h == 1) {  // O is still: the product with this half waits for this warp
+#pragma unroll 1
+              for (int e = 0; e < D; e += 16) {
+                uint32_t o[16];
+                tmem_ld16(o_at + e, o);
+                tmem_wait_ld();
+                pin(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st16(o_at + e, o);
+              }
+            }
+            weights(0);
+            weights(1);
           }
-          tmem_st16(s_at + 32 * half + 16 * c, w);
+          l += sum[0] + sum[1];
+          tmem_st16(s_at + 32 * h, w[0]);
+          tmem_st16(s_at + 32 * h + 16, w[1]);
+          if (h == 0) {
+            tmem_ld32(s_at + 64, v[0]);
+            tmem_ld32(s_at + 96, v[1]);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_p(t, h));
         }
-        const float2 both = unpack2(sum);
-        l += both.x + both.y;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p(t));
-        ++npv;
       }
       // ---- the tile's result
-      if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (npv - 1) & 1, abort_s, 9);
-      if (ok && nk > 0) {
-        *mine_s = l;
-        ok = meet();
-        if (ok) l = half ? *other_s + l : l + *other_s;
-        ok = ok && meet();  // (both have read)
-      }
+      if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (ns - 1) & 1, abort_s, 9);
       tc_fence_after();
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      const bool mine = token < u.lq;
+      const bool mine = token < u.lq, bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
 #pragma unroll 1
-      for (int c = 0; c < D / 2; c += 16) {
+      for (int c = 0; c < D; c += 16) {
         uint32_t o[16] = {};
         if (ok && nk > 0) {
           tmem_ld16(o_at + c, o);
           tmem_wait_ld();
+          pin(o);
         }
         if (!mine) continue;
-        uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + D / 2 * half + c);
+        uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + c);
 #pragma unroll
         for (int i = 0; i < 16; i += 8) {
           uint32_t w[4];
@@ -402,7 +416,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
             // (a row without keys has what another unit left in O)
             const float x = l > 0.f ? __uint_as_float(o[i + 2 * e]) * inv : 0.f, y = l > 0.f ? __uint_as_float(o[i + 2 * e + 1]) * inv : 0.f;
             const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-            w[e] = ok && !isnan(l) ? *reinterpret_cast<const uint32_t*>(&h) : 0x7fff7fffu;
+            w[e] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
           }
           dst[i >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -412,8 +426,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_of(t));
       }
-      if (mine && half == 0) {
-        const float e = !ok || isnan(l) ? NAN : (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY);
+      if (mine) {
+        const float e = bad ? NAN : (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY);
         if (a.lse) a.lse[at] = e;
         const int w = token - (u.lq - a.W);
         if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
@@ -422,7 +436,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 17) {
+  if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }

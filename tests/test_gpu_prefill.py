@@ -90,6 +90,33 @@ def test_rising_and_falling_maxima():
         _check(q, k, v, out, lse, 0)
 
 
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 2, 1), (64, 4, 2), (128, 1, 1)])
+@pytest.mark.parametrize("places", ["every tile", "one key", "few rows"])
+def test_maxima_that_rise_far(d, Hq, Hkv, places):
+    # by more than fp32 exponentials of one reference can bridge: rows have to take new ones on the way
+    n = 900
+    q, k, v = _draw(n, n, Hq, Hkv, d, 19)
+    u = torch.randn(d, device="cuda")
+    u /= u.norm()
+    size = torch.full((n,), 30.0, device="cuda")
+    ramp = torch.linspace(0, 600, n, device="cuda")
+    if places == "one key":    # in the second half of a tile; later tiles fall back
+        ramp = torch.zeros(n, device="cuda")
+        ramp[[200, 333, 500]] = torch.tensor([90.0, 200.0, 600.0], device="cuda")
+    if places == "few rows":
+        size = torch.where(torch.arange(n, device="cuda") % 37 == 5, 40.0, 0.0)
+    q = (q + size[:, None, None] * u).to(torch.bfloat16)
+    k = (k + ramp[:, None, None] * u).to(torch.bfloat16)
+    out, lse, _ = sk.snapkv_prefill_attention(q, k, v, [n])
+    _check(q, k, v, out, lse, 0)
+    again = sk.snapkv_prefill_attention(q, k, v, [n])
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+    # and those that fall as far
+    k = k.flip(0)
+    out, lse, _ = sk.snapkv_prefill_attention(q, k, v, [n])
+    _check(q, k, v, out, lse, 0)
+
+
 def test_the_same_bits_every_run_and_in_every_batch():
     q, k, v, out, lse = _run([700, 130], [700, 130], 8, 2, 128, 4)
     again = sk.snapkv_prefill_attention(q, k, v, [700, 130])
