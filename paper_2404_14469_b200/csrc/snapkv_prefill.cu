@@ -262,9 +262,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         if (u.most == 1) tc_commit(bar_qe);
         for (int j = 0; ok && j < u.most; ++j, use += 2) {
           const bool more = j + 1 < u.most;
-          ok = full(use + 1) && (!more || full(use + 2));
           for (int t = 0; ok && t < 2; ++t) {
-            if (j < u.nk[t]) ok = values(t, use + 1, j == 0);
+            if (t == 0) ok = full(use + 1);
+            if (ok && j < u.nk[t]) ok = values(t, use + 1, j == 0);
+            if (ok && t == 0 && more) ok = full(use + 2);
             if (ok && j + 1 < u.nk[t]) ok = scores(t, use + 2);
           }
           if (!ok) break;
