@@ -271,6 +271,30 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N) {
          | (static_cast<uint32_t>(M >> 4) << 24); // M
 }
 
+// Asks for a block of this grid that has not started yet, to do its work in its place: 16 bytes of
+// answer arrive at `dst` (16-byte aligned) and as many are completed on the barrier.  After an answer
+// without a block no further one may be asked for.
+__device__ __forceinline__ void next_block_ask(uint32_t dst, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(dst),
+               "r"(bar)
+               : "memory");
+}
+// The block's index (of a one-dimensional grid), or -1.
+__device__ __forceinline__ int next_block_answer(uint32_t src) {
+  unsigned long long lo, hi;
+  asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(lo), "=l"(hi) : "r"(src) : "memory");
+  int x;
+  asm volatile(
+      "{\n\t.reg .b128 a;\n\t.reg .pred p;\n\t"
+      "mov.b128 a, {%1, %2};\n\t"
+      "mov.b32 %0, -1;\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
+      : "=r"(x)
+      : "l"(lo), "l"(hi));
+  return x;
+}
+
 // True in exactly one lane of a converged warp.  Unlike a test of the lane index, the
 // compiler knows the guarded region runs in a single thread.
 __device__ __forceinline__ bool elect_one() {

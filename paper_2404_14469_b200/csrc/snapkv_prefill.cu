@@ -15,8 +15,10 @@
 // over the first key tile and moves only when later weights pass 2^64, which shows in their sum.  The
 // row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
 // in two halves, so that the product with V runs while the second one is computed.
-// Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  Persistent: a block's next unit has its
-// keys on the way while the present one is written out.
+// Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
+// sequences and their last queries first, and a running block takes over the next one that has not
+// started (so the next unit's keys are on the way while the present one is written out, and blocks end
+// together: with a fixed assignment eight prompts of 200 to 4000 tokens took 255 us, now NOW_MIXED).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -33,6 +35,7 @@ namespace {
 
 constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
 constexpr int PF_THREADS = 320;
+constexpr int PF_ASKED = 4;       // answers about next units that are kept
 constexpr int PF_KEYS = 128;      // keys per tile
 // A row takes a new reference when 64 of its weights add up to more than 2^64 (PF_FAR).  That loses
 // nothing: weights and their sums are floating-point numbers, far from fp32's and bf16's 2^127.
@@ -67,10 +70,11 @@ struct PfSmem {
   static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
   static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
   // full[STAGES], empty[STAGES], q_full, q_empty, then per tile: S, the halves of P, the product with
-  // the first of them, the whole product, O read out; and drain
-  static constexpr int NBAR = 2 * STAGES + 2 + 12 + 1;
+  // the first of them, the whole product, O read out; drain; answers about the next unit there and read
+  static constexpr int NBAR = 2 * STAGES + 2 + 12 + 1 + 2 * PF_ASKED;
   static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
-  static constexpr int DYN_BYTES = OFF_MISC + 16 + 1024;
+  static constexpr int OFF_ANSWER = OFF_MISC + 16, OFF_CLOSED = OFF_ANSWER + 16 * PF_ASKED;
+  static constexpr int DYN_BYTES = OFF_CLOSED + 16 + 1024;
   static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
 };
 
@@ -120,6 +124,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   auto bar_pv = [&](int t) { return bar_qe + 8u * (9 + t); };
   auto bar_of = [&](int t) { return bar_qe + 8u * (11 + t); };
   const uint32_t bar_drain = bar_qe + 8u * 13;
+  auto bar_there = [&](int i) { return bar_qe + 8u * (14 + i); };
+  auto bar_read = [&](int i) { return bar_qe + 8u * (14 + PF_ASKED + i); };
+  auto answer = [&](int i) { return sbase + SM::OFF_ANSWER + 16u * i; };
+  volatile int* closed_s = reinterpret_cast<volatile int*>(smem + SM::OFF_CLOSED);  // -1, in the end the number of answers
   volatile uint32_t* tmem_ptr_s = reinterpret_cast<volatile uint32_t*>(smem + SM::OFF_MISC);
   volatile int* abort_s = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -141,6 +149,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       mbar_init(bar_of(t), 4);
     }
     mbar_init(bar_drain, 1);
+    for (int i = 0; i < PF_ASKED; ++i) {
+      mbar_init(bar_there(i), 1);
+      mbar_init(bar_read(i), 9);  // MMA and eight softmax warps
+    }
+    *closed_s = -1;
     *abort_s = 0;
     *reinterpret_cast<volatile unsigned long long*>(abort_s + 1) = a.wait_ns;
     mbar_fence_init();
@@ -156,12 +169,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   const uint32_t tmem = *tmem_ptr_s;
 
   const int tok_log2 = 7 - a.pack_log2, tile_tokens = 1 << tok_log2;
-  // The unit that the block takes in round r: the list begins with the longest, and every other round
-  // runs backwards, so that no block gets the longer one of every round.
-  auto unit_at = [&](int r, Unit* u) {
-    const int c = static_cast<int>(blockIdx.x), G = static_cast<int>(gridDim.x);
-    const int i = r * G + (r & 1 ? G - 1 - c : c);
-    if (i >= a.units) return false;
+  auto unit_of = [&](int i, Unit* u) {
     int s = 0;
     while (s + 1 < a.nseq && i >= seqs.s[s + 1].unit0) ++s;
     const PrefillSeq& q = seqs.s[s];
@@ -179,7 +187,18 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       u->nk[t] = last < first ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
     }
     u->most = max(u->nk[0], u->nk[1]);
-    return true;
+  };
+  // Unit r of the block, for the roles: its own, then those that it takes over.
+  auto thread_unit = [&](int r, Unit* u) {
+    int i = static_cast<int>(blockIdx.x);
+    if (r > 0) {
+      const int at = (r - 1) % PF_ASKED;
+      if (!mbar_wait_thread(bar_there(at), (r - 1) / PF_ASKED & 1, abort_s, 11)) return false;
+      i = next_block_answer(answer(at));
+      if (warp == 9) mbar_arrive(bar_read(at));
+    }
+    if (i >= 0) unit_of(i, u);
+    return i >= 0;
   };
   Unit u;
 
@@ -188,7 +207,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     if (elect_one()) {
       int fill = 0, nq = 0;
       bool ok = true;
-      for (int r = 0; ok && unit_at(r, &u); ++r) {
+      int asked = 0;
+      for (int r = 0; ok && thread_unit(r, &u); ++r) {
+        ok = mbar_wait_thread(bar_read(r % PF_ASKED), (r / PF_ASKED & 1) ^ 1, abort_s, 12);
+        if (!ok) break;
+        mbar_expect_tx(bar_there(r % PF_ASKED), 16);
+        next_block_ask(answer(r % PF_ASKED), bar_there(r % PF_ASKED));
+        ++asked;
         if (u.most == 0) continue;
         const int kv = u.head0 / a.g;
         auto load = [&](const CUtensorMap* m, int j) {
@@ -213,7 +238,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       if (*abort_s != 0) {  // never leave with copies in flight
         if (nq) drain(bar_qf, (nq - 1) & 1, a.wait_ns);
         for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
+        if (asked) drain(bar_there((asked - 1) % PF_ASKED), (asked - 1) / PF_ASKED & 1, a.wait_ns);
       }
+      *closed_s = asked;
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA
@@ -252,7 +279,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         ++npv[t];
         return true;
       };
-      for (int r = 0; ok && unit_at(r, &u); ++r) {
+      for (int r = 0; ok && thread_unit(r, &u); ++r) {
         if (u.most == 0) continue;
         ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7) && full(use);
         for (int t = 0; ok && t < 2; ++t)
@@ -287,7 +314,27 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     const unsigned long long scale2 = pack2(a.c2, a.c2);
     int ns = 0;  // key tiles so far
     bool ok = true;
-    for (int r = 0; unit_at(r, &u); ++r) {
+    // Unit r again.  After a wait that gave up the units that the block has taken are filled with NaN:
+    // the answers that there are, once it is known how many.
+    auto warp_unit = [&](int r, Unit* u) {
+      int i = static_cast<int>(blockIdx.x);
+      if (r > 0) {
+        const int at = (r - 1) % PF_ASKED;
+        ok = ok && mbar_wait_warp(bar_there(at), (r - 1) / PF_ASKED & 1, abort_s, 11);
+        if (!ok) {
+          const unsigned long long t0 = globaltimer_ns();
+          bool waiting = true;
+          while (waiting) waiting = __any_sync(0xffffffffu, *closed_s < 0 && globaltimer_ns() - t0 < 4 * a.wait_ns);
+          if (__any_sync(0xffffffffu, r > *closed_s)) return false;
+        }
+        i = next_block_answer(answer(at));
+        __syncwarp();
+        if (ok && lane == 0) mbar_arrive(bar_read(at));
+      }
+      if (i >= 0) unit_of(i, u);
+      return i >= 0;
+    };
+    for (int r = 0; warp_unit(r, &u); ++r) {
       const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
@@ -453,8 +500,7 @@ cudaError_t launch_prefill(const CUtensorMap& tmQ, const PrefillArgs& a, const P
     if (e != cudaSuccess) return e;
     ready.set();
   }
-  const int grid = a.units < sm_count() ? a.units : sm_count();
-  return launch_pdl(kernel, dim3(grid), dim3(PF_THREADS), SMEM, stream, tmQ, a, seqs);
+  return launch_pdl(kernel, dim3(a.units), dim3(PF_THREADS), SMEM, stream, tmQ, a, seqs);
 }
 
 bool strides_ok(const int64_t* s, int d) {
