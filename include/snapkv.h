@@ -401,7 +401,7 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
  *   q_starts     HOST int64 [B] or NULL: the first token of each sequence in q and in the outputs,
  *                ascending and without overlap; NULL: one sequence behind the other.  k_starts likewise
  *                for k and v (any order, overlaps allowed: common prefixes).
- *   out          bf16 device, dense [tokens, Hq, d]: softmax_j(q_i.k_j / sqrt(d)) v_j
+ *   out          bf16 device, dense [tokens, Hq, d], 32-byte aligned: softmax_j(q_i.k_j / sqrt(d)) v_j
  *   out_lse      fp32 device, dense [tokens, Hq], or NULL: natural log of sum_j exp(q_i.k_j / sqrt(d))
  *   lse_obs      fp32 device, dense [B, Hq, W]: the same of each sequence's last W queries; NULL with
  *                W = 0.  W <= 128, and with W > 0 every sequence needs W queries.

@@ -12,7 +12,7 @@
 //   the end.
 // What bounds the kernel is a tile's chain: S, its weights, P.V, and no S before that as P lies over it.
 // So the weights do not wait for a maximum, and none is taken: the reference m of a row is its maximum
-// over the first key tile and moves only when later weights pass 2^64, which shows in their sum.  The
+// over the first 32 keys and moves only when later weights pass 2^64, which shows in their sum.  The
 // row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
 // in two halves, so that the product with V runs while the second one is computed.
 // Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
@@ -84,6 +84,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, 
       "[%0], [%1, {%3, %4, %5}], [%2];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
+}
+
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 
 // Wait for a copy or an MMA that is in flight, when the abort flag is set already.
@@ -358,18 +364,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           for (int i = 1; i < 32; ++i) y = fmaxf(y, x[i]);
           return y;
         };
-        if (j == 0) {  // the reference: the row's maximum over the first tile
-          float top = -INFINITY;
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            float x[32];
-            tmem_ld32(s_at + 32 * c, x);
-            tmem_wait_ld();
-            pin(x);
-            mask(x, c);
-            top = fmaxf(top, largest(x));
-          }
-          m = top == -INFINITY ? 0.f : top * a.c2;  // (no key in sight, or none that weighs anything)
+        if (j == 0) {  // the reference: 0 where no key is in sight, or none that weighs anything
+          float x[32];
+          tmem_ld32(s_at, x);
+          tmem_wait_ld();
+          pin(x);
+          mask(x, 0);
+          const float top = largest(x);
+          m = top == -INFINITY ? 0.f : top * a.c2;
         }
         // Half of the keys at a time: their scores are on the way while the first half is worked on.
         float v[2][32];
@@ -446,6 +448,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       const float inv = l > 0.f ? 1.f / l : 0.f;
       const bool mine = token < u.lq, bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
+      // (a row per lane: 32-byte stores write whole sectors and take half of the passes through the
+      // load/store unit that 16-byte ones do)
 #pragma unroll 1
       for (int c = 0; c < D; c += 16) {
         uint32_t o[16] = {};
@@ -455,19 +459,15 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           pin(o);
         }
         if (!mine) continue;
-        uint4* dst = reinterpret_cast<uint4*>(a.out + at * D + c);
+        uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            // (a row without keys has what another unit left in O)
-            const float x = l > 0.f ? __uint_as_float(o[i + 2 * e]) * inv : 0.f, y = l > 0.f ? __uint_as_float(o[i + 2 * e + 1]) * inv : 0.f;
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-            w[e] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
-          }
-          dst[i >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int e = 0; e < 8; ++e) {
+          // (a row without keys has what another unit left in O)
+          const float x = l > 0.f ? __uint_as_float(o[2 * e]) * inv : 0.f, y = l > 0.f ? __uint_as_float(o[2 * e + 1]) * inv : 0.f;
+          const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+          w[e] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
         }
+        st_global_32(a.out + at * D + c, w);
       }
       if (ok && nk > 0) {
         tc_fence_before();
@@ -558,8 +558,9 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
   if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || d < 1 || W < 0 || !q_lens) return SNAPKV_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || W > 128 || Hq > 65535) return SNAPKV_ERR_UNSUPPORTED;
   if (!q || !k || !v || !out || (W > 0) != (lse_obs != nullptr)) return SNAPKV_ERR_INVALID_ARG;
-  for (const void* p : {q, k, v, static_cast<const void*>(out)})
+  for (const void* p : {q, k, v})
     if (reinterpret_cast<uintptr_t>(p) & 15) return SNAPKV_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(out) & 31) return SNAPKV_ERR_INVALID_ARG;  // (32-byte stores)
   if ((reinterpret_cast<uintptr_t>(out_lse) | reinterpret_cast<uintptr_t>(lse_obs)) & 3) return SNAPKV_ERR_INVALID_ARG;
   const int64_t dq[2] = {static_cast<int64_t>(Hq) * d, d}, dk[2] = {static_cast<int64_t>(Hkv) * d, d};
   const int64_t *qs = q_strides ? q_strides : dq, *ks = k_strides ? k_strides : dk, *vs = v_strides ? v_strides : dk;
