@@ -18,7 +18,7 @@
 // Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
 // sequences and their last queries first, and a running block takes over the next one that has not
 // started (so the next unit's keys are on the way while the present one is written out, and blocks end
-// together: with a fixed assignment eight prompts of 200 to 4000 tokens took 255 us, now NOW_MIXED).
+// together: with a fixed assignment eight prompts of 200 to 4000 tokens took 253 us, then 240).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -57,6 +57,7 @@ struct PrefillArgs {
   int Hq, g, W, nseq, units;
   int pack_log2;       // query heads per tile
   int head_packs;      // Hq >> pack_log2
+  int tiles_log2;      // query tiles per unit: 1 << tiles_log2
   float c2;            // log2(e) / sqrt(d)
   unsigned long long wait_ns;
   __nv_bfloat16* out;
@@ -179,7 +180,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     int s = 0;
     while (s + 1 < a.nseq && i >= seqs.s[s + 1].unit0) ++s;
     const PrefillSeq& q = seqs.s[s];
-    const int blocks = (q.lq + 2 * tile_tokens - 1) >> (tok_log2 + 1);
+    const int unit_log2 = tok_log2 + a.tiles_log2, blocks = (q.lq + (1 << unit_log2) - 1) >> unit_log2;
     const int at = i - q.unit0, from_end = at / a.head_packs;
     u->seq = s;
     u->lq = q.lq;
@@ -187,10 +188,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     u->q0 = q.q0;
     u->n0 = q.lk - q.lq;
     u->head0 = (at - from_end * a.head_packs) << a.pack_log2;
-    u->token0 = (blocks - 1 - from_end) << (tok_log2 + 1);
+    u->token0 = (blocks - 1 - from_end) << unit_log2;
     for (int t = 0; t < 2; ++t) {
       const int first = u->token0 + t * tile_tokens, last = min(first + tile_tokens, q.lq) - 1;
-      u->nk[t] = last < first ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
+      u->nk[t] = last < first || t >> a.tiles_log2 ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
     }
     u->most = max(u->nk[0], u->nk[1]);
   };
@@ -446,7 +447,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (ns - 1) & 1, abort_s, 9);
       tc_fence_after();
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      const bool mine = token < u.lq, bad = !ok || isnan(l);
+      const bool mine = token < u.lq && !(t >> a.tiles_log2), bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
       // (a row per lane: 32-byte stores write whole sectors and take half of the passes through the
       // load/store unit that 16-byte ones do)
@@ -524,12 +525,23 @@ template <int MAPS>
 cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ, const SeqSpan* span, int n, cudaStream_t stream) {
   using u64 = unsigned long long;
   PrefillSeqs<MAPS> seqs = {};
-  const int tok = 2 << (7 - a.pack_log2);
+  // One tile per unit where that leaves every unit an SM of its own: a tile alone is through its chain
+  // sooner than two that take turns (a 1K prompt of four heads of 64: 15.1 us, 17.9 with two).
+  auto count = [&](int tiles_log2) {
+    long long c = 0;
+    for (int i = 0; i < n; ++i) {
+      const int log2 = 7 - a.pack_log2 + tiles_log2;
+      c += static_cast<long long>((span[i].lq + (1ll << log2) - 1) >> log2) * a.head_packs;
+    }
+    return c;
+  };
+  a.tiles_log2 = count(0) <= sm_count() ? 0 : 1;
+  const int tok = (1 << a.tiles_log2) << (7 - a.pack_log2);
   long long units = 0;
   for (int i = 0; i < n; ++i) {
     const SeqSpan& p = span[i];
     seqs.s[i] = PrefillSeq{p.lq, p.lk, static_cast<int>(units), p.batch, p.q0};
-    units += static_cast<long long>((p.lq + tok - 1) / tok) * a.head_packs;
+    units += (static_cast<long long>(p.lq) + tok - 1) / tok * a.head_packs;
     const u64 dims[3] = {static_cast<u64>(c.d), static_cast<u64>(p.lk > 0 ? p.lk : 1), static_cast<u64>(c.Hkv)};
     const u64 ks[2] = {static_cast<u64>(c.ks[0]) * 2, static_cast<u64>(c.ks[1]) * 2},
               vs[2] = {static_cast<u64>(c.vs[0]) * 2, static_cast<u64>(c.vs[1]) * 2};
@@ -565,7 +577,7 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
   const int64_t dq[2] = {static_cast<int64_t>(Hq) * d, d}, dk[2] = {static_cast<int64_t>(Hkv) * d, d};
   const int64_t *qs = q_strides ? q_strides : dq, *ks = k_strides ? k_strides : dk, *vs = v_strides ? v_strides : dk;
   if (!strides_ok(qs, d) || !strides_ok(ks, d) || !strides_ok(vs, d)) return SNAPKV_ERR_INVALID_ARG;
-  constexpr int64_t MAX_TOKENS = 1ll << 31;
+  constexpr int64_t MAX_TOKENS = 1ll << 30;
   int64_t q_end = 0, k_end = 0;
   for (int b = 0; b < B; ++b) {
     const int lq = q_lens[b], lk = k_lens ? k_lens[b] : lq;
@@ -576,7 +588,6 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
     k_end = k0 + lk;
     if (q_end > MAX_TOKENS || k_end > MAX_TOKENS) return SNAPKV_ERR_INVALID_ARG;
   }
-  // (sizes beyond these would leave 32-bit coordinates and unit numbers)
   PrefillArgs a = {};
   a.Hq = Hq, a.g = Hq / Hkv, a.W = W;
   while (a.pack_log2 < 6 && a.g % (2 << a.pack_log2) == 0) ++a.pack_log2;
