@@ -318,11 +318,16 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         for (int i = 0; i < 2; ++i)
           qb[k][i] = h < gc ? __ldg(reinterpret_cast<const uint32_t*>(qh + k * 16 + i * 8)) : 0u;
     }
-    float acc[KS][4];  // dimensions 16 j + gid (+ 8) of columns 2 tig, 2 tig + 1
+    // Dimensions 16 j + gid (+ 8) of columns 2 tig, 2 tig + 1.  The matrix instructions cut what they add
+    // instead of rounding it, which adds up to 2e-6 of a result over a hundred tiles: every FLUSH tiles
+    // their sums go to others that are rounded (5e-7 then, at no cost that shows).
+    constexpr int FLUSH = 8;
+    float acc[KS][4], sums[KS][4];
 #pragma unroll
     for (int j = 0; j < KS; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+      for (int i = 0; i < 4; ++i) acc[j][i] = sums[j][i] = 0.f;
+    int flush = FLUSH;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of columns 2 tig + {0, 1}; l: this lane's keys
     for (int t = cur.t0; t < cur.t1 && !failed; ++t) {
       const int s = n % DP_STAGES;
@@ -368,6 +373,8 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             for (int j = 0; j < KS; ++j) {
               acc[j][c] *= corr;
               acc[j][c + 2] *= corr;
+              sums[j][c] *= corr;
+              sums[j][c + 2] *= corr;
             }
             m[c] = mn;
           }
@@ -405,7 +412,21 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       }
       __syncwarp();  // every lane has read the stage
       request();
+      if (--flush == 0) {
+        flush = FLUSH;
+#pragma unroll
+        for (int j = 0; j < KS; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sums[j][i] += acc[j][i];
+            acc[j][i] = 0.f;
+          }
+      }
     }
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] += sums[j][i];
     if (failed) l[0] = l[1] = NAN;  // the outputs of this unit and of those behind it become NaN
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
