@@ -35,7 +35,7 @@ namespace {
 
 constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
 constexpr int PF_THREADS = 320;
-constexpr int PF_ASKED = 4;       // answers about next units that are kept
+constexpr int PF_UNITS = 4;       // units that the TMA thread may be ahead
 constexpr int PF_KEYS = 128;      // keys per tile
 // A row takes a new reference when 64 of its weights add up to more than 2^64 (PF_FAR).  That loses
 // nothing: weights and their sums are floating-point numbers, far from fp32's and bf16's 2^127.
@@ -64,21 +64,6 @@ struct PrefillArgs {
   float *lse, *lse_obs;
 };
 
-template <int D>
-struct PfSmem {
-  static constexpr int COLS = D / 64;
-  static constexpr int TILE = COLS * PF_BLOCK;          // one tile of Q, K or V
-  static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
-  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
-  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile: S, the halves of P, the product with
-  // the first of them, the whole product, O read out; drain; answers about the next unit there and read
-  static constexpr int NBAR = 2 * STAGES + 2 + 12 + 1 + 2 * PF_ASKED;
-  static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
-  static constexpr int OFF_ANSWER = OFF_MISC + 16, OFF_CLOSED = OFF_ANSWER + 16 * PF_ASKED;
-  static constexpr int DYN_BYTES = OFF_CLOSED + 16 + 1024;
-  static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
-};
-
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
@@ -94,21 +79,40 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
 }
 
 // Wait for a copy or an MMA that is in flight, when the abort flag is set already.
-__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+__device__ __forceinline__ bool drain(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
   const unsigned long long t0 = globaltimer_ns();
   while (!mbar_try_wait(bar, parity))
-    if (globaltimer_ns() - t0 > limit_ns) return;
+    if (globaltimer_ns() - t0 > limit_ns) return false;
+  return true;
 }
 
-// What a block knows of a unit.
-struct Unit {
+// What a block knows of a unit.  The TMA thread works it out, ahead of the others, and leaves it in
+// shared memory (each role for itself took 2000 clocks between two units).
+struct __align__(16) Unit {
   int seq, lq, batch;
   int n0;         // keys in front of the first query (may be negative)
   int head0;      // first query head
   int token0;     // first token of tile 0
-  long long q0;
   int nk[2];      // key tiles of each query tile
-  int most;
+  long long q0;
+  int most;       // of nk; -1: there is no further unit
+};
+
+template <int D>
+struct PfSmem {
+  static constexpr int COLS = D / 64;
+  static constexpr int TILE = COLS * PF_BLOCK;          // one tile of Q, K or V
+  static constexpr int STAGES = D == 128 ? 5 : 8;       // ring of K and V tiles
+  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
+  // full[STAGES], empty[STAGES], q_full, q_empty, then per tile: S, the halves of P, the product with
+  // the first of them, the whole product, O read out; drain; the answer about the next block; units
+  // there and read
+  static constexpr int NBAR = 2 * STAGES + 2 + 12 + 2 + 2 * PF_UNITS;
+  static constexpr int OFF_MISC = OFF_BAR + ((NBAR * 8 + 15) & ~15);  // tensor memory, abort flag, wait limit
+  static constexpr int OFF_UNIT = OFF_MISC + 16, OFF_ANSWER = OFF_UNIT + PF_UNITS * sizeof(Unit);
+  static constexpr int OFF_CLOSED = OFF_ANSWER + 16;
+  static constexpr int DYN_BYTES = OFF_CLOSED + 16 + 1024;
+  static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
 };
 
 template <int D, int MAPS>
@@ -131,10 +135,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   auto bar_pv = [&](int t) { return bar_qe + 8u * (9 + t); };
   auto bar_of = [&](int t) { return bar_qe + 8u * (11 + t); };
   const uint32_t bar_drain = bar_qe + 8u * 13;
-  auto bar_there = [&](int i) { return bar_qe + 8u * (14 + i); };
-  auto bar_read = [&](int i) { return bar_qe + 8u * (14 + PF_ASKED + i); };
-  auto answer = [&](int i) { return sbase + SM::OFF_ANSWER + 16u * i; };
-  volatile int* closed_s = reinterpret_cast<volatile int*>(smem + SM::OFF_CLOSED);  // -1, in the end the number of answers
+  const uint32_t bar_answer = bar_drain + 8u, answer = sbase + SM::OFF_ANSWER;
+  auto bar_there = [&](int i) { return bar_answer + 8u * (1 + i); };
+  auto bar_read = [&](int i) { return bar_answer + 8u * (1 + PF_UNITS + i); };
+  Unit* units_s = reinterpret_cast<Unit*>(smem + SM::OFF_UNIT);
+  volatile int* closed_s = reinterpret_cast<volatile int*>(smem + SM::OFF_CLOSED);  // -1, in the end the number of units
   volatile uint32_t* tmem_ptr_s = reinterpret_cast<volatile uint32_t*>(smem + SM::OFF_MISC);
   volatile int* abort_s = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -156,7 +161,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       mbar_init(bar_of(t), 4);
     }
     mbar_init(bar_drain, 1);
-    for (int i = 0; i < PF_ASKED; ++i) {
+    mbar_init(bar_answer, 1);
+    for (int i = 0; i < PF_UNITS; ++i) {
       mbar_init(bar_there(i), 1);
       mbar_init(bar_read(i), 9);  // MMA and eight softmax warps
     }
@@ -195,18 +201,6 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     }
     u->most = max(u->nk[0], u->nk[1]);
   };
-  // Unit r of the block, for the roles: its own, then those that it takes over.
-  auto thread_unit = [&](int r, Unit* u) {
-    int i = static_cast<int>(blockIdx.x);
-    if (r > 0) {
-      const int at = (r - 1) % PF_ASKED;
-      if (!mbar_wait_thread(bar_there(at), (r - 1) / PF_ASKED & 1, abort_s, 11)) return false;
-      i = next_block_answer(answer(at));
-      if (warp == 9) mbar_arrive(bar_read(at));
-    }
-    if (i >= 0) unit_of(i, u);
-    return i >= 0;
-  };
   Unit u;
 
   if (warp == 8) {
@@ -214,13 +208,36 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     if (elect_one()) {
       int fill = 0, nq = 0;
       bool ok = true;
-      int asked = 0;
-      for (int r = 0; ok && thread_unit(r, &u); ++r) {
-        ok = mbar_wait_thread(bar_read(r % PF_ASKED), (r / PF_ASKED & 1) ^ 1, abort_s, 12);
+      // A unit for the others to see; its place is free once the unit PF_UNITS in front has been read.
+      int shown = 0, asked = 0, pending = -1;  // units shown, blocks asked for, a unit taken but not shown
+      bool ended = false;
+      auto show = [&] {
+        units_s[shown % PF_UNITS] = u;
+        mbar_arrive(bar_there(shown % PF_UNITS));
+        ++shown;
+      };
+      for (int i = static_cast<int>(blockIdx.x); i >= 0;) {
+        if (asked) {
+          ok = mbar_wait_thread(bar_answer, (asked - 1) & 1, abort_s, 11);
+          if (!ok) break;
+          i = next_block_answer(answer);
+        }
+        ended = i < 0;
+        pending = i;
+        if (ended) {
+          u.most = -1;
+        } else {
+          fence_proxy_async();  // the last answer has been read
+          mbar_expect_tx(bar_answer, 16);
+          next_block_ask(answer, bar_answer);
+          ++asked;
+          unit_of(i, &u);
+        }
+        ok = mbar_wait_thread(bar_read(shown % PF_UNITS), (shown / PF_UNITS & 1) ^ 1, abort_s, 12);
         if (!ok) break;
-        mbar_expect_tx(bar_there(r % PF_ASKED), 16);
-        next_block_ask(answer(r % PF_ASKED), bar_there(r % PF_ASKED));
-        ++asked;
+        show();
+        pending = -1;
+        if (ended) break;
         if (u.most == 0) continue;
         const int kv = u.head0 / a.g;
         auto load = [&](const CUtensorMap* m, int j) {
@@ -241,13 +258,24 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
                         static_cast<int>(u.q0) + u.token0 + t * tile_tokens);
         ++nq;
         for (int j = 0; ok && j < u.most; ++j) ok = load(&seqs.k[u.seq], j) && load(&seqs.v[u.seq], j);
+        if (!ok) break;
       }
       if (*abort_s != 0) {  // never leave with copies in flight
         if (nq) drain(bar_qf, (nq - 1) & 1, a.wait_ns);
         for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
-        if (asked) drain(bar_there((asked - 1) % PF_ASKED), (asked - 1) / PF_ASKED & 1, a.wait_ns);
+        // blocks that this one has taken over, or asked for and got, are filled with NaN, too
+        if (!ended && drain(bar_answer, (asked - 1) & 1, a.wait_ns)) {
+          const int last = next_block_answer(answer);
+          for (int e = 0; e < 2; ++e) {
+            const int i = e == 0 ? pending : last;
+            if (i < 0) continue;
+            unit_of(i, &u);
+            drain(bar_read(shown % PF_UNITS), (shown / PF_UNITS & 1) ^ 1, a.wait_ns);
+            show();
+          }
+        }
       }
-      *closed_s = asked;
+      *closed_s = shown;
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA
@@ -286,7 +314,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         ++npv[t];
         return true;
       };
-      for (int r = 0; ok && thread_unit(r, &u); ++r) {
+      for (int r = 0; ok; ++r) {
+        ok = mbar_wait_thread(bar_there(r % PF_UNITS), r / PF_UNITS & 1, abort_s, 11);
+        if (!ok) break;
+        u = units_s[r % PF_UNITS];
+        mbar_arrive(bar_read(r % PF_UNITS));
+        if (u.most < 0) break;
         if (u.most == 0) continue;
         ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7) && full(use);
         for (int t = 0; ok && t < 2; ++t)
@@ -321,27 +354,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     const unsigned long long scale2 = pack2(a.c2, a.c2);
     int ns = 0;  // key tiles so far
     bool ok = true;
-    // Unit r again.  After a wait that gave up the units that the block has taken are filled with NaN:
-    // the answers that there are, once it is known how many.
-    auto warp_unit = [&](int r, Unit* u) {
-      int i = static_cast<int>(blockIdx.x);
-      if (r > 0) {
-        const int at = (r - 1) % PF_ASKED;
-        ok = ok && mbar_wait_warp(bar_there(at), (r - 1) / PF_ASKED & 1, abort_s, 11);
-        if (!ok) {
-          const unsigned long long t0 = globaltimer_ns();
-          bool waiting = true;
-          while (waiting) waiting = __any_sync(0xffffffffu, *closed_s < 0 && globaltimer_ns() - t0 < 4 * a.wait_ns);
-          if (__any_sync(0xffffffffu, r > *closed_s)) return false;
+    for (int r = 0;; ++r) {
+      const int at_unit = r % PF_UNITS;
+      ok = ok && mbar_wait_warp(bar_there(at_unit), r / PF_UNITS & 1, abort_s, 11);
+      if (!ok) {  // a wait gave up: what units there still are become NaN, once it is known how many
+        const unsigned long long t0 = globaltimer_ns();
+        while (__any_sync(0xffffffffu, *closed_s < 0 && globaltimer_ns() - t0 < 8 * a.wait_ns)) {
+          if (__all_sync(0xffffffffu, mbar_try_wait(bar_there(at_unit), r / PF_UNITS & 1))) break;
         }
-        i = next_block_answer(answer(at));
-        __syncwarp();
-        if (ok && lane == 0) mbar_arrive(bar_read(at));
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bar_there(at_unit), r / PF_UNITS & 1))) break;
       }
-      if (i >= 0) unit_of(i, u);
-      return i >= 0;
-    };
-    for (int r = 0; warp_unit(r, &u); ++r) {
+      u = units_s[at_unit];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_read(at_unit));
+      if (u.most < 0) break;
       const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
@@ -449,15 +475,25 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       const float inv = l > 0.f ? 1.f / l : 0.f;
       const bool mine = token < u.lq && !(t >> a.tiles_log2), bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
+      if (mine) {
+        const float e = bad ? NAN : (l > 0.f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY);
+        if (a.lse) a.lse[at] = e;
+        const int w = token - (u.lq - a.W);
+        if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
+      }
       // (a row per lane: 32-byte stores write whole sectors and take half of the passes through the
       // load/store unit that 16-byte ones do)
+      uint32_t o[16] = {}, ahead[16] = {};
+      const bool there = ok && nk > 0;
+      if (there) tmem_ld16(o_at, ahead);
 #pragma unroll 1
       for (int c = 0; c < D; c += 16) {
-        uint32_t o[16] = {};
-        if (ok && nk > 0) {
-          tmem_ld16(o_at + c, o);
+        if (there) {
           tmem_wait_ld();
-          pin(o);
+          pin(ahead);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = ahead[e];
+          if (c + 16 < D) tmem_ld16(o_at + c + 16, ahead);
         }
         if (!mine) continue;
         uint32_t w[8];
@@ -474,12 +510,6 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_of(t));
-      }
-      if (mine) {
-        const float e = bad ? NAN : (l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY);
-        if (a.lse) a.lse[at] = e;
-        const int w = token - (u.lq - a.W);
-        if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
       }
     }
   }
