@@ -445,7 +445,7 @@ snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const voi
  *                 device, dense [T, Hq, d], the queries turned like the keys.
  *   k_pool ...    the pools as in snapkv_compress_paged, written here, with Hc heads: cache head c gets
  *                 key head c / (Hc / Hkv) (Hc = Hkv, or Hc = Hq for caches with one selection per
- *                 query head).  Any page_size >= 1.
+ *                 query head).  Any page_size >= 1; a sequence has less than 2^31 - 64 rows.
  * With inv_freq = NULL this copies a dense compressed cache [B, Hc, rows, d] (strides {Hc * rows * d, d,
  * rows * d}) into pages.  A row beyond the table, or whose table entry lies outside [0, num_pages), is
  * dropped.  Two tokens must not share a cache row.  All else in the pools stays as it is.
@@ -473,7 +473,9 @@ snapkv_status_t snapkv_append_paged(const void* k_new, const void* v_new, const 
  *               without rows gets zeros and a log-sum-exp of minus infinity.
  *   out         fp32 device, dense [B, Hq, d];  out_lse fp32 device [B, Hq] or NULL.
  * What lies in a page behind a sequence's last row is never used (it may be anything).  Accuracy and
- * reproducibility as in snapkv_decode_attention.  `workspace`: device memory of
+ * reproducibility as in snapkv_decode_attention.  One kernel.  A block waits for partial results of blocks
+ * in front of it, which have started before it and wait for nobody; a wait that exceeds its limit makes
+ * the affected outputs NaN.  pages_per_seq * page_size < 2^31 - 64 (SNAPKV_ERR_UNSUPPORTED).  `workspace`: device memory of
  * snapkv_decode_paged_workspace_size bytes (0: arguments not acceptable), 256-byte aligned, nothing in it
  * has to be initialised; calls that may overlap on the GPU need one each.  B * Hq <= 65535.
  */

@@ -205,7 +205,8 @@ extern "C" snapkv_status_t snapkv_append_paged(const void* k_new, const void* v_
   if (B < 1 || T < 0 || Hkv < 1 || Hc < 1 || Hc % Hkv != 0 || d < 1 || pages_per_seq < 1 || page_size < 1 ||
       num_pages < 1 || (!cu_tokens && T % B != 0) || (q && Hq < 1))
     return SNAPKV_ERR_INVALID_ARG;
-  if (d != 64 && d != 128) return SNAPKV_ERR_UNSUPPORTED;
+  if ((d != 64 && d != 128) || static_cast<long long>(pages_per_seq) * page_size >= (1ll << 31) - 64)
+    return SNAPKV_ERR_UNSUPPORTED;
   if (!k_new || !v_new || !cache_lens || !k_pool || !v_pool || !page_table || (q && (!inv_freq || !q_out)))
     return SNAPKV_ERR_INVALID_ARG;
   if (inv_freq && (rot < 2 || rot > d || rot % 2 != 0)) return SNAPKV_ERR_INVALID_ARG;

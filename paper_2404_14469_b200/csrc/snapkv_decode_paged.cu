@@ -367,7 +367,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             const float mn = fmaxf(m[c], mx[c]);
-            const float corr = m[c] == -INFINITY ? 0.f : exp2f(m[c] - mn);  // (nothing summed yet: 0)
+            const float corr = ex2_approx(m[c] - mn);  // (nothing summed yet: 0)
             l[c] *= corr;
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
@@ -379,9 +379,11 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             m[c] = mn;
           }
         }
-        // (a subtile past the last row, possible for 32-row tiles, has no key: p = 0)
+        // (no key yet, as in a subtile past the last row of a 32-row tile: p = 0, whatever the reference;
+        // a NaN stays one)
+        const float ref[2] = {fmaxf(m[0], -1e30f), fmaxf(m[1], -1e30f)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = m[i & 1] == -INFINITY ? 0.f : exp2f(p[i] - m[i & 1]);
+        for (int i = 0; i < 4; ++i) p[i] = ex2_approx(p[i] - ref[i & 1]);
         l[0] += p[0] + p[2];
         l[1] += p[1] + p[3];
         uint32_t lo3[3], hi3[3];  // terms of keys gid and gid + 8

@@ -608,12 +608,13 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
   const int64_t *qs = q_strides ? q_strides : dq, *ks = k_strides ? k_strides : dk, *vs = v_strides ? v_strides : dk;
   if (!strides_ok(qs, d) || !strides_ok(ks, d) || !strides_ok(vs, d)) return SNAPKV_ERR_INVALID_ARG;
   constexpr int64_t MAX_TOKENS = 1ll << 30;
-  int64_t q_end = 0, k_end = 0;
+  int64_t q_end = 0, k_end = 0, queries = 0;
   for (int b = 0; b < B; ++b) {
     const int lq = q_lens[b], lk = k_lens ? k_lens[b] : lq;
     if (lq < 0 || lk < 0 || lq < W) return SNAPKV_ERR_INVALID_ARG;
     const int64_t q0 = q_starts ? q_starts[b] : q_end, k0 = k_starts ? k_starts[b] : k_end;
     if (q0 < q_end || q0 > MAX_TOKENS || k0 < 0 || k0 > MAX_TOKENS) return SNAPKV_ERR_INVALID_ARG;
+    queries += lq;
     q_end = q0 + lq;
     k_end = k0 + lk;
     if (q_end > MAX_TOKENS || k_end > MAX_TOKENS) return SNAPKV_ERR_INVALID_ARG;
@@ -626,7 +627,7 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
   a.wait_ns = wait_limit_setting();
   a.out = static_cast<__nv_bfloat16*>(out);
   a.lse = out_lse, a.lse_obs = lse_obs;
-  if (q_end == 0) return SNAPKV_OK;
+  if (queries == 0) return SNAPKV_OK;
   CUtensorMap tmQ;
   {
     using u64 = unsigned long long;
