@@ -12,7 +12,7 @@
 //   the end.
 // What bounds the kernel is a tile's chain: S, its weights, P.V, and no S before that as P lies over it.
 // So the weights do not wait for a maximum, and none is taken: the reference m of a row is its maximum
-// over the first 32 keys and moves only when later weights pass 2^64, which shows in their sum.  The
+// over the first 32 keys and moves only when later weights pass 2^32, which shows in their sum.  The
 // row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
 // in two halves, so that the product with V runs while the second one is computed.
 // Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
@@ -37,9 +37,9 @@ constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
 constexpr int PF_THREADS = 320;
 constexpr int PF_UNITS = 4;       // units that the TMA thread may be ahead
 constexpr int PF_KEYS = 128;      // keys per tile
-// A row takes a new reference when 64 of its weights add up to more than 2^64 (PF_FAR).  That loses
-// nothing: weights and their sums are floating-point numbers, far from fp32's and bf16's 2^127.
-constexpr float PF_FAR = 18446744073709551616.f;
+// A row takes a new reference when 64 of its weights add up to more than 2^32 (PF_FAR).  That loses
+// nothing: weights and their sums are floating-point numbers, far from the 2^127 of fp32 and bf16.
+constexpr float PF_FAR = 4294967296.f;
 constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
 
 struct PrefillSeq {
