@@ -3,7 +3,7 @@
 //   out_i = sum_j p_ij v_j / l_i,  p_ij = exp(s_ij - m_i),  s_ij = q_i.k_j / sqrt(d),  j <= Lk - Lq + i
 // with m_i a reference near the running maximum and l_i the running sum; lse_i = m_i + ln l_i.
 //
-// One work unit: two tiles of 128 query rows that share their keys.  Of a group's query heads the
+// One work unit: two tiles of 128 query rows that share their keys (one in the SPLIT form, see there).  Of a group's query heads the
 // largest power of two that divides the group is packed into a tile, (token, head) with the head
 // fastest: 32 tokens of 4 heads instead of 128 of one, so that a unit's two tiles need the same keys
 // but for a few.  Both products run on tcgen05 over 128 keys at a time:
@@ -57,7 +57,6 @@ struct PrefillArgs {
   int Hq, g, W, nseq, units;
   int pack_log2;       // query heads per tile
   int head_packs;      // Hq >> pack_log2
-  int tiles_log2;      // query tiles per unit: 1 << tiles_log2
   float c2;            // log2(e) / sqrt(d)
   unsigned long long wait_ns;
   __nv_bfloat16* out;
@@ -115,7 +114,10 @@ struct PfSmem {
   static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one block");
 };
 
-template <int D, int MAPS>
+// SPLIT: for a few units.  A unit is one query tile, whose key tiles the two softmax warpgroups take in
+// turn, each with a reference, a sum and an O of its own; in the end the second hands its results to the
+// first through the ring's memory.  A block has one unit then.
+template <int D, int MAPS, bool SPLIT>
 __global__ void __launch_bounds__(PF_THREADS, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, const __grid_constant__ PrefillSeqs<MAPS> seqs) {
   using SM = PfSmem<D>;
@@ -186,7 +188,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     int s = 0;
     while (s + 1 < a.nseq && i >= seqs.s[s + 1].unit0) ++s;
     const PrefillSeq& q = seqs.s[s];
-    const int unit_log2 = tok_log2 + a.tiles_log2, blocks = (q.lq + (1 << unit_log2) - 1) >> unit_log2;
+    const int unit_log2 = tok_log2 + (SPLIT ? 0 : 1), blocks = (q.lq + (1 << unit_log2) - 1) >> unit_log2;
     const int at = i - q.unit0, from_end = at / a.head_packs;
     u->seq = s;
     u->lq = q.lq;
@@ -196,8 +198,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
     u->head0 = (at - from_end * a.head_packs) << a.pack_log2;
     u->token0 = (blocks - 1 - from_end) << unit_log2;
     for (int t = 0; t < 2; ++t) {
-      const int first = u->token0 + t * tile_tokens, last = min(first + tile_tokens, q.lq) - 1;
-      u->nk[t] = last < first || t >> a.tiles_log2 ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
+      const int first = u->token0 + (SPLIT ? 0 : t * tile_tokens), last = min(first + tile_tokens, q.lq) - 1;
+      u->nk[t] = last < first ? 0 : (max(u->n0 + last + 1, 0) + PF_KEYS - 1) / PF_KEYS;
+      if (SPLIT) u->nk[t] = (u->nk[t] + 1 - t) / 2;  // every other one
     }
     u->most = max(u->nk[0], u->nk[1]);
   };
@@ -217,7 +220,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         ++shown;
       };
       for (int i = static_cast<int>(blockIdx.x); i >= 0;) {
-        if (asked) {
+        if (SPLIT && shown) {
+          i = -1;
+        } else if (asked) {
           ok = mbar_wait_thread(bar_answer, (asked - 1) & 1, abort_s, 11);
           if (!ok) break;
           i = next_block_answer(answer);
@@ -226,6 +231,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         pending = i;
         if (ended) {
           u.most = -1;
+        } else if (SPLIT) {
+          unit_of(i, &u);
         } else {
           fence_proxy_async();  // the last answer has been read
           mbar_expect_tx(bar_answer, 16);
@@ -251,20 +258,29 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         };
         ok = mbar_wait_thread(bar_qe, (nq & 1) ^ 1, abort_s, 2);
         if (!ok) break;
-        mbar_expect_tx(bar_qf, 2 * TILE);
-        for (int t = 0; t < 2; ++t)
+        constexpr int QT = SPLIT ? 1 : 2;
+        mbar_expect_tx(bar_qf, QT * TILE);
+        for (int t = 0; t < QT; ++t)
           for (int c = 0; c < COLS; ++c)
             tma_load_3d(q_s + t * TILE + c * PF_BLOCK, &tmQ, bar_qf, c * 64, u.head0,
                         static_cast<int>(u.q0) + u.token0 + t * tile_tokens);
         ++nq;
-        for (int j = 0; ok && j < u.most; ++j) ok = load(&seqs.k[u.seq], j) && load(&seqs.v[u.seq], j);
+        for (int j = 0; ok && j < u.most; ++j) {
+          if constexpr (SPLIT) {
+            const bool two = j < u.nk[1];
+            ok = load(&seqs.k[u.seq], 2 * j) && (!two || load(&seqs.k[u.seq], 2 * j + 1)) && load(&seqs.v[u.seq], 2 * j) &&
+                 (!two || load(&seqs.v[u.seq], 2 * j + 1));
+          } else {
+            ok = load(&seqs.k[u.seq], j) && load(&seqs.v[u.seq], j);
+          }
+        }
         if (!ok) break;
       }
       if (*abort_s != 0) {  // never leave with copies in flight
         if (nq) drain(bar_qf, (nq - 1) & 1, a.wait_ns);
         for (int i = fill > STAGES ? fill - STAGES : 0; i < fill; ++i) drain(bar_full(i % STAGES), i / STAGES & 1, a.wait_ns);
         // blocks that this one has taken over, or asked for and got, are filled with NaN, too
-        if (!ended && drain(bar_answer, (asked - 1) & 1, a.wait_ns)) {
+        if (!ended && asked && drain(bar_answer, (asked - 1) & 1, a.wait_ns)) {
           const int last = next_block_answer(answer);
           for (int e = 0; e < 2; ++e) {
             const int i = e == 0 ? pending : last;
@@ -287,7 +303,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       auto scores = [&](int t, int i) {  // S of tile t with the keys of ring entry i
         // P of the tile before lies over it: that product must be through
         if (npv[t] > 0 && !mbar_wait_thread(bar_pv(t), (npv[t] - 1) & 1, abort_s, 4)) return false;
-        const uint64_t qd = umma_desc_k128(q_s + t * TILE), kd = umma_desc_k128(kv_s + (i % STAGES) * TILE);
+        const uint64_t qd = umma_desc_k128(q_s + (SPLIT ? 0 : t * TILE)), kd = umma_desc_k128(kv_s + (i % STAGES) * TILE);
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -321,7 +337,28 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         mbar_arrive(bar_read(r % PF_UNITS));
         if (u.most < 0) break;
         if (u.most == 0) continue;
-        ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7) && full(use);
+        ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7);
+        if constexpr (SPLIT) {
+          // ring entries of step j: its one or two key tiles, then as many value tiles
+          auto key = [&](int t, int j) { return use + 4 * j + t; };
+          auto value = [&](int t, int j) { return use + 4 * j + (j < u.nk[1] ? 2 : 1) + t; };
+          auto score = [&](int t, int j) {
+            if (!full(key(t, j)) || !scores(t, key(t, j))) return false;
+            tc_commit(bar_empty(key(t, j) % STAGES));
+            return true;
+          };
+          for (int j = -1; ok && j < u.most; ++j)
+            for (int t = 0; ok && t < 2; ++t) {
+              if (j >= 0 && j < u.nk[t]) {
+                ok = full(value(t, j)) && values(t, value(t, j), j == 0);
+                if (ok) tc_commit(bar_empty(value(t, j) % STAGES));
+              }
+              if (ok && j + 1 < u.nk[t]) ok = score(t, j + 1);
+            }
+          use += 2 * (u.nk[0] + u.nk[1]);
+          continue;
+        }
+        ok = ok && full(use);
         for (int t = 0; ok && t < 2; ++t)
           if (u.nk[t] > 0) ok = scores(t, use);
         if (!ok) break;
@@ -368,19 +405,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_read(at_unit));
       if (u.most < 0) break;
-      const int token = u.token0 + t * tile_tokens + (row >> a.pack_log2);
+      const int token = u.token0 + (SPLIT ? 0 : t * tile_tokens) + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
       const int jmax = u.n0 + min(token, u.lq - 1);             // the last key that the row sees
-      const int jfree = u.n0 + u.token0 + t * tile_tokens;      // every row of the tile sees keys up to here
+      const int jfree = u.n0 + u.token0 + (SPLIT ? 0 : t * tile_tokens);  // every row of the tile sees keys up to here
       float m = 0.f, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m)
       for (int j = 0; ok && j < nk; ++j, ++ns) {
         ok = mbar_wait_warp(bar_s(t), ns & 1, abort_s, 8);
         if (!ok) break;
         tc_fence_after();
+        const int key0 = (SPLIT ? 2 * j + t : j) * PF_KEYS;
         auto mask = [&](float (&x)[32], int c) {
-          if (j * PF_KEYS + PF_KEYS - 1 > jfree) {
-            const int see = jmax - j * PF_KEYS - 32 * c;
+          if (key0 + PF_KEYS - 1 > jfree) {
+            const int see = jmax - key0 - 32 * c;
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = i <= see ? x[i] : -INFINITY;
           }
@@ -431,7 +469,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           weights(0);
           weights(1);
           if (__any_sync(0xffffffffu, sum[0] + sum[1] > PF_FAR)) {
-            // A row passed its reference by far: a new one, by a power of two (P rescales exactly).
+            // A row passed its reference by far: a new one, by a power of two.
             const bool move = sum[0] + sum[1] > PF_FAR;
             const float top = fmaxf(largest(v[0]), largest(v[1])) * a.c2;
             const float up = move ? ceilf(top - m) : 0.f, f = ex2_approx(-up);
@@ -472,8 +510,45 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       // ---- the tile's result
       if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (ns - 1) & 1, abort_s, 9);
       tc_fence_after();
+      // SPLIT: what the second warpgroup has, [element][row] and a maximum and a sum per row
+      float* theirs = reinterpret_cast<float*>(smem + SM::OFF_KV) + row;
+      float f_own = 1.f, f_their = 0.f;
+      if constexpr (SPLIT) {
+        if (t == 1) {
+          if (nk == 0) continue;
+          // (the ring is free when the first one's last product is through as well)
+          ok = ok && mbar_wait_warp(bar_pv(0), (u.nk[0] - 1) & 1, abort_s, 9);
+          if (!ok) continue;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t x[16];
+            tmem_ld16(o_at + c, x);
+            tmem_wait_ld();
+            pin(x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) theirs[(c + e) * 128] = __uint_as_float(x[e]);
+          }
+          theirs[D * 128] = m;
+          theirs[(D + 1) * 128] = l;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_of(1));
+          continue;
+        }
+        if (ok && u.nk[1] > 0) {
+          ok = mbar_wait_warp(bar_of(1), 0, abort_s, 9);
+          const float m1 = theirs[D * 128], l1 = theirs[(D + 1) * 128];
+          if (ok && l1 != 0.f) {  // (a row that sees none of their keys has no maximum there)
+            const float top = fmaxf(m, m1);
+            f_own = ex2_approx(m - top);
+            f_their = ex2_approx(m1 - top);
+            l = l * f_own + l1 * f_their;
+            m = top;
+          }
+        }
+      }
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      const bool mine = token < u.lq && !(t >> a.tiles_log2), bad = !ok || isnan(l);
+      const bool mine = token < u.lq, bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
       if (mine) {
         const float e = bad ? NAN : (l > 0.f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY);
@@ -496,6 +571,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           if (c + 16 < D) tmem_ld16(o_at + c + 16, ahead);
         }
         if (!mine) continue;
+        if constexpr (SPLIT) {
+          if (f_their != 0.f)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              o[e] = __float_as_uint(__uint_as_float(o[e]) * f_own + theirs[(c + e) * 128] * f_their);
+        }
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -521,9 +602,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
   }
 }
 
-template <int D, int MAPS>
+template <int D, int MAPS, bool SPLIT>
 cudaError_t launch_prefill(const CUtensorMap& tmQ, const PrefillArgs& a, const PrefillSeqs<MAPS>& seqs, cudaStream_t stream) {
-  auto kernel = prefill_kernel<D, MAPS>;
+  auto kernel = prefill_kernel<D, MAPS, SPLIT>;
   constexpr int SMEM = PfSmem<D>::DYN_BYTES;
   static DeviceOnce ready;
   if (!ready.done()) {
@@ -555,18 +636,12 @@ template <int MAPS>
 cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ, const SeqSpan* span, int n, cudaStream_t stream) {
   using u64 = unsigned long long;
   PrefillSeqs<MAPS> seqs = {};
-  // One tile per unit where that leaves every unit an SM of its own: a tile alone is through its chain
-  // sooner than two that take turns (a 1K prompt of four heads of 64: 15.1 us, 17.9 with two).
-  auto count = [&](int tiles_log2) {
-    long long c = 0;
-    for (int i = 0; i < n; ++i) {
-      const int log2 = 7 - a.pack_log2 + tiles_log2;
-      c += static_cast<long long>((span[i].lq + (1ll << log2) - 1) >> log2) * a.head_packs;
-    }
-    return c;
-  };
-  a.tiles_log2 = count(0) <= sm_count() ? 0 : 1;
-  const int tok = (1 << a.tiles_log2) << (7 - a.pack_log2);
+  // One tile per unit and its keys in two halves where that leaves every unit an SM of its own: the
+  // chain is half as long (a 1K prompt of four heads of 64: 12.4 us; with two tiles per unit 17.9, with one 15.1).
+  long long tiles = 0;
+  for (int i = 0; i < n; ++i) tiles += (span[i].lq + (128ll >> a.pack_log2) - 1) / (128 >> a.pack_log2) * a.head_packs;
+  const bool split = tiles <= sm_count();
+  const int tok = (split ? 1 : 2) << (7 - a.pack_log2);
   long long units = 0;
   for (int i = 0; i < n; ++i) {
     const SeqSpan& p = span[i];
@@ -584,7 +659,9 @@ cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ,
   a.nseq = n;
   a.units = static_cast<int>(units);
   if (units == 0) return cudaSuccess;
-  return c.d == 128 ? launch_prefill<128, MAPS>(tmQ, a, seqs, stream) : launch_prefill<64, MAPS>(tmQ, a, seqs, stream);
+  auto f = c.d == 128 ? (split ? launch_prefill<128, MAPS, true> : launch_prefill<128, MAPS, false>)
+                      : (split ? launch_prefill<64, MAPS, true> : launch_prefill<64, MAPS, false>);
+  return f(tmQ, a, seqs, stream);
 }
 
 }  // namespace
