@@ -406,7 +406,7 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
  *   lse_obs      fp32 device, dense [B, Hq, W]: the same of each sequence's last W queries; NULL with
  *                W = 0.  W <= 128, and with W > 0 every sequence needs W queries.
  * No sequence may begin or end behind token 2^30.
- * A query that sees no key gets zeros and minus infinity.  Rows of q, out and out_lse that belong to no
+ * A query that sees no key, or whose scores are all minus infinity, gets zeros and minus infinity.  Rows of q, out and out_lse that belong to no
  * sequence are not touched; a sequence's keys and values reach its own queries only, whatever they hold.
  * (Inside a sequence an infinity or NaN in a VALUE row may reach queries in front of it, too.)
  * Products of bf16 accumulated in fp32, softmax statistics in fp32, probabilities rounded to bf16 for

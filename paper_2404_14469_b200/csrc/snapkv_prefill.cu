@@ -12,7 +12,8 @@
 //   the end.
 // What bounds the kernel is a tile's chain: S, its weights, P.V, and no S before that as P lies over it.
 // So the weights do not wait for a maximum, and none is taken: the reference m of a row is its maximum
-// over the first 32 keys and moves only when later weights pass 2^32, which shows in their sum.  The
+// over the first 32 keys (rounded up to a whole power of two) and moves only when later weights pass 2^32,
+// which shows in their sum: to the maximum of those keys, wherever the old one was.  The
 // row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
 // in two halves, so that the product with V runs while the second one is computed.
 // Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
@@ -22,6 +23,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -40,6 +42,8 @@ constexpr int PF_KEYS = 128;      // keys per tile
 // A row takes a new reference when 64 of its weights add up to more than 2^32 (PF_FAR).  That loses
 // nothing: weights and their sums are floating-point numbers, far from the 2^127 of fp32 and bf16.
 constexpr float PF_FAR = 4294967296.f;
+constexpr float PF_WIDE = 16777216.f;  // 2^24
+constexpr float PF_NONE = -3e38f;      // the reference of a row that has none yet: any finite score is far above it
 constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
 
 struct PrefillSeq {
@@ -409,19 +413,28 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
       const int nk = u.nk[t];
       const int jmax = u.n0 + min(token, u.lq - 1);             // the last key that the row sees
-      const int jfree = u.n0 + u.token0 + (SPLIT ? 0 : t * tile_tokens);  // every row of the tile sees keys up to here
-      float m = 0.f, l = 0.f;  // reference in the log2 domain, sum of exp2(. - m)
+      int jfree = u.n0 + u.token0 + (SPLIT ? 0 : t * tile_tokens);  // every row of the tile sees keys up to here
+      // The row's reference in the log2 domain is m + far * c2, l the sum of exp2(. - reference).  m is a
+      // whole number, so that a weight's exponent is rounded once (fma) and references differ by powers of
+      // two.  From PF_WIDE on m would be coarser than one: there the score itself is the reference (far),
+      // subtracted from the others before they are scaled, and m is 0.
+      float m = PF_NONE, far = 0.f, l = 0.f;
+      auto refer = [&](bool set, float top) {
+        const float x = ceilf(top * a.c2);
+        const bool is_far = fabsf(x) >= PF_WIDE;
+        m = set ? (is_far ? 0.f : x) : m;
+        far = set ? (is_far ? top : 0.f) : far;
+        if (__any_sync(0xffffffffu, far != 0.f)) jfree = INT_MIN;  // (the far rows' subtraction is with the masks)
+      };
       for (int j = 0; ok && j < nk; ++j, ++ns) {
         ok = mbar_wait_warp(bar_s(t), ns & 1, abort_s, 8);
         if (!ok) break;
         tc_fence_after();
         const int key0 = (SPLIT ? 2 * j + t : j) * PF_KEYS;
         auto mask = [&](float (&x)[32], int c) {
-          if (key0 + PF_KEYS - 1 > jfree) {
-            const int see = jmax - key0 - 32 * c;
+          const int see = jmax - key0 - 32 * c;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = i <= see ? x[i] : -INFINITY;
-          }
+          for (int i = 0; i < 32; ++i) x[i] = i <= see ? x[i] : -INFINITY;
         };
         auto largest = [&](const float (&x)[32]) {
           float y = x[0];
@@ -429,14 +442,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           for (int i = 1; i < 32; ++i) y = fmaxf(y, x[i]);
           return y;
         };
-        if (j == 0) {  // the reference: 0 where no key is in sight, or none that weighs anything
+        if (j == 0) {  // the reference: none yet where no key is in sight, or none that weighs anything
           float x[32];
           tmem_ld32(s_at, x);
           tmem_wait_ld();
           pin(x);
-          mask(x, 0);
+          if (key0 + PF_KEYS - 1 > jfree) mask(x, 0);
           const float top = largest(x);
-          m = top == -INFINITY ? 0.f : top * a.c2;
+          refer(top != -INFINITY, top);
         }
         // Half of the keys at a time: their scores are on the way while the first half is worked on.
         float v[2][32];
@@ -447,8 +460,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           tmem_wait_ld();
           pin(v[0]);
           pin(v[1]);
-          mask(v[0], 2 * h);
-          mask(v[1], 2 * h + 1);
+          if (key0 + PF_KEYS - 1 > jfree) {  // (with a branch for each a batch of 64-wide heads took 161 us, with one 158)
+            mask(v[0], 2 * h);
+            mask(v[1], 2 * h + 1);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[0][i] -= far, v[1][i] -= far;
+          }
           uint32_t w[2][16];
           float sum[2];
           auto weights = [&](int c) {
@@ -469,11 +486,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           weights(0);
           weights(1);
           if (__any_sync(0xffffffffu, sum[0] + sum[1] > PF_FAR)) {
-            // A row passed its reference by far: a new one, by a power of two.
+            // A row passed its reference by far, or had none: a new one.
             const bool move = sum[0] + sum[1] > PF_FAR;
-            const float top = fmaxf(largest(v[0]), largest(v[1])) * a.c2;
-            const float up = move ? ceilf(top - m) : 0.f, f = ex2_approx(-up);
-            m += up;
+            if (__any_sync(0xffffffffu, far != 0.f)) {  // the scores themselves (this half's columns hold them until its weights are stored)
+              tmem_ld32(s_at + 64 * h, v[0]);
+              tmem_ld32(s_at + 64 * h + 32, v[1]);
+              tmem_wait_ld();
+              pin(v[0]);
+              pin(v[1]);
+              mask(v[0], 2 * h);
+              mask(v[1], 2 * h + 1);
+            }
+            const float m_was = m, far_was = far;
+            refer(move, fmaxf(largest(v[0]), largest(v[1])));
+            const float f = move ? ex2_approx(fmaf(far_was - far, a.c2, m_was - m)) : 1.f;
             l *= f;
             if (h == 1) {  // the first half of P is handed over: its product must be through
               ok = mbar_wait_warp(bar_ph(t), ns & 1, abort_s, 9);
@@ -491,6 +517,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
                 tmem_st16(o_at + e, o);
               }
             }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[0][i] -= far, v[1][i] -= far;
             weights(0);
             weights(1);
           }
@@ -510,7 +538,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       // ---- the tile's result
       if (ok && nk > 0) ok = mbar_wait_warp(bar_pv(t), (ns - 1) & 1, abort_s, 9);
       tc_fence_after();
-      // SPLIT: what the second warpgroup has, [element][row] and a maximum and a sum per row
+      // SPLIT: what the second warpgroup has, [element][row], a reference and a sum per row
       float* theirs = reinterpret_cast<float*>(smem + SM::OFF_KV) + row;
       float f_own = 1.f, f_their = 0.f;
       if constexpr (SPLIT) {
@@ -530,20 +558,21 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
             for (int e = 0; e < 16; ++e) theirs[(c + e) * 128] = __uint_as_float(x[e]);
           }
           theirs[D * 128] = m;
-          theirs[(D + 1) * 128] = l;
+          theirs[(D + 1) * 128] = far;
+          theirs[(D + 2) * 128] = l;
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_of(1));
           continue;
         }
         if (ok && u.nk[1] > 0) {
           ok = mbar_wait_warp(bar_of(1), 0, abort_s, 9);
-          const float m1 = theirs[D * 128], l1 = theirs[(D + 1) * 128];
-          if (ok && l1 != 0.f) {  // (a row that sees none of their keys has no maximum there)
-            const float top = fmaxf(m, m1);
-            f_own = ex2_approx(m - top);
-            f_their = ex2_approx(m1 - top);
+          const float m1 = theirs[D * 128], far1 = theirs[(D + 1) * 128], l1 = theirs[(D + 2) * 128];
+          if (ok && l1 != 0.f) {  // (a row that sees none of their keys has no reference there)
+            const float above = fmaf(far - far1, a.c2, m - m1);  // of the own reference over theirs
+            f_own = ex2_approx(fminf(above, 0.f));
+            f_their = ex2_approx(fminf(-above, 0.f));
             l = l * f_own + l1 * f_their;
-            m = top;
+            if (above < 0.f) m = m1, far = far1;
           }
         }
       }
@@ -551,7 +580,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       const bool mine = token < u.lq, bad = !ok || isnan(l);
       const long long at = (u.q0 + token) * a.Hq + head;
       if (mine) {
-        const float e = bad ? NAN : (l > 0.f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY);
+        const float e = bad ? NAN : (l > 0.f ? (fmaf(far, a.c2, m) + __log2f(l)) * 0.6931471805599453f : -INFINITY);
         if (a.lse) a.lse[at] = e;
         const int w = token - (u.lq - a.W);
         if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
