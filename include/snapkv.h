@@ -410,8 +410,8 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
  * sequence are not touched; a sequence's keys and values reach its own queries only, whatever they hold.
  * (Inside a sequence an infinity or NaN in a VALUE row may reach queries in front of it, too.)
  * Products of bf16 accumulated in fp32, softmax statistics in fp32, probabilities rounded to bf16 for
- * the product with V (they are at most 1 and their sum is taken before), results reproducible from run
- * to run.  The host arrays are read during the call.  No workspace; one launch for every 32 sequences.
+ * the product with V (their sum is taken before).  The sum over the values is divided last: results are
+ * right as long as (Lk + 64) max|v| is a number of fp32.  Results are reproducible from run to run.  The host arrays are read during the call.  No workspace; one launch for every 32 sequences.
  * A kernel wait that exceeds its limit makes the affected rows NaN.
  */
 snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const void* v,

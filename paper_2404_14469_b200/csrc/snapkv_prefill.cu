@@ -12,8 +12,8 @@
 //   the end.
 // What bounds the kernel is a tile's chain: S, its weights, P.V, and no S before that as P lies over it.
 // So the weights do not wait for a maximum, and none is taken: the reference m of a row is its maximum
-// over the first 32 keys (rounded up to a whole power of two) and moves only when later weights pass 2^32,
-// which shows in their sum: to the maximum of those keys, wherever the old one was.  The
+// over the first 32 keys, with some room (PF_ROOM), and moves only when later weights pass it, which
+// shows in their sum: to the maximum of those keys, wherever the old one was.  The
 // row's thread then rescales what it has under the old reference, in TMEM too.  And P is handed over
 // in two halves, so that the product with V runs while the second one is computed.
 // Warps: 0-3 softmax of tile 0, 4-7 of tile 1, 8 TMA, 9 MMA.  The grid has a block per unit, longest
@@ -39,9 +39,13 @@ constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
 constexpr int PF_THREADS = 320;
 constexpr int PF_UNITS = 4;       // units that the TMA thread may be ahead
 constexpr int PF_KEYS = 128;      // keys per tile
-// A row takes a new reference when 64 of its weights add up to more than 2^32 (PF_FAR).  That loses
-// nothing: weights and their sums are floating-point numbers, far from the 2^127 of fp32 and bf16.
-constexpr float PF_FAR = 4294967296.f;
+// A row's reference is 2^10 (PF_ROOM) above the keys that it was taken from, and the row takes a new one
+// when 64 of its weights add up to more than 64 (PF_FAR).  So the sums are at most what a running maximum
+// gives, (Lk + 64) and (Lk + 64) max|v|, and logits may rise by 2^10 to 2^16 without a new reference.  (The
+// room costs nothing but the smallest 2^-10 of the number range.  With sums that may pass what the reference
+// was taken from by 2^16, 2^10 and 2^7, mixed prompts of 64-wide heads took 156, 158 and 212 us, a 32K
+// prompt 7.61, 7.63 and 8.43 ms.)
+constexpr float PF_FAR = 64.f, PF_ROOM = 10.f;
 constexpr float PF_WIDE = 16777216.f;  // 2^24
 constexpr float PF_NONE = -3e38f;      // the reference of a row that has none yet: any finite score is far above it
 constexpr int PF_BLOCK = 128 * 128;  // bytes of 128 rows of 64 elements, 128-byte swizzled
@@ -417,12 +421,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       // The row's reference in the log2 domain is m + far * c2, l the sum of exp2(. - reference).  m is a
       // whole number, so that a weight's exponent is rounded once (fma) and references differ by powers of
       // two.  From PF_WIDE on m would be coarser than one: there the score itself is the reference (far),
-      // subtracted from the others before they are scaled, and m is 0.
+      // subtracted from the others before they are scaled, and m is the room.
       float m = PF_NONE, far = 0.f, l = 0.f;
       auto refer = [&](bool set, float top) {
         const float x = ceilf(top * a.c2);
         const bool is_far = fabsf(x) >= PF_WIDE;
-        m = set ? (is_far ? 0.f : x) : m;
+        m = set ? (is_far ? PF_ROOM : x + PF_ROOM) : m;
         far = set ? (is_far ? top : 0.f) : far;
         if (__any_sync(0xffffffffu, far != 0.f)) jfree = INT_MIN;  // (the far rows' subtraction is with the masks)
       };
@@ -486,7 +490,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           weights(0);
           weights(1);
           if (__any_sync(0xffffffffu, sum[0] + sum[1] > PF_FAR)) {
-            // A row passed its reference by far, or had none: a new one.
+            // A row passed its reference, or had none: a new one.
             const bool move = sum[0] + sum[1] > PF_FAR;
             if (__any_sync(0xffffffffu, far != 0.f)) {  // the scores themselves (this half's columns hold them until its weights are stored)
               tmem_ld32(s_at + 64 * h, v[0]);
