@@ -470,7 +470,8 @@ snapkv_status_t snapkv_append_paged(const void* k_new, const void* v_new, const 
  *               as rows of zeros.
  *   seq_lens    DEVICE int32 [B]: rows of each cache, the new token's own among them; may change between
  *               replays of a captured graph.  Clamped to [0, pages_per_seq * page_size]; a sequence
- *               without rows gets zeros and a log-sum-exp of minus infinity.
+ *               without rows, or a head whose scores are all minus infinity, gets zeros and a log-sum-exp
+ *               of minus infinity.
  *   out         fp32 device, dense [B, Hq, d];  out_lse fp32 device [B, Hq] or NULL.
  * What lies in a page behind a sequence's last row is never used (it may be anything).  Accuracy and
  * reproducibility as in snapkv_decode_attention.  One kernel.  A block waits for partial results of blocks

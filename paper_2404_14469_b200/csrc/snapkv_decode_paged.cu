@@ -45,6 +45,9 @@ constexpr int DP_MAX_GRID = MAX_GRID;
 // shares are equal in tiles and units.  (64 sequences of 20 to 300 rows: 14.9 us with 1, 14.0 with 2,
 // 13.8 with 3; of 30 to 8000 rows 62.7, 61.9, 62.1.)
 constexpr int DP_UNIT_COST = 2;
+// References are at least this: below any score that is a number (scaled, in the log2 domain, 0.18 of fp32's range), so
+// that scores of minus infinity weigh nothing and minus infinity is not subtracted from itself.
+constexpr float DP_FLOOR = -1e38f;
 
 constexpr int dp_tile_rows(int D) { return DP_STAGE_BYTES / (4 * D); }
 
@@ -367,7 +370,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             const float mn = fmaxf(m[c], mx[c]);
-            const float corr = ex2_approx(m[c] - mn);  // (nothing summed yet: 0)
+            const float corr = ex2_approx(m[c] - fmaxf(mn, DP_FLOOR));  // (nothing summed yet: 0)
             l[c] *= corr;
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
@@ -381,7 +384,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         }
         // (no key yet, as in a subtile past the last row of a 32-row tile: p = 0, whatever the reference;
         // a NaN stays one)
-        const float ref[2] = {fmaxf(m[0], -1e30f), fmaxf(m[1], -1e30f)};
+        const float ref[2] = {fmaxf(m[0], DP_FLOOR), fmaxf(m[1], DP_FLOOR)};
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = ex2_approx(p[i] - ref[i & 1]);
         l[0] += p[0] + p[2];
@@ -451,7 +454,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
           const int h = 2 * tig + c;
           if (h >= gc) continue;
           const size_t bh = static_cast<size_t>(cur.b) * a.Hq + head * a.g + h0 + h;
-          const float inv = 1.f / l[c];
+          const float inv = l[c] == 0.f ? 0.f : 1.f / l[c];
 #pragma unroll
           for (int j = 0; j < KS; ++j) {
             a.out[bh * D + 16 * j + gid] = acc[j][c] * inv;
@@ -514,7 +517,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       auto part = [&](int k) { return parts + (k == 0 ? i : 2 * (w + k)) * PART; };
       const int mine = lane & 7;
       const float mk = mine < count ? part(mine)[h] : -INFINITY;
-      float M = fmaxf(mk, -1e30f), L = 0.f, o[E] = {};
+      float M = fmaxf(mk, DP_FLOOR), L = 0.f, o[E] = {};
 #pragma unroll
       for (int x = 1; x < 8; x <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
       const float f = ex2_approx(mk - M);
@@ -528,7 +531,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       }
       if (complete) {
         const size_t bh = static_cast<size_t>(u.b) * a.Hq + head * a.g + h0 + h;
-        const float inv = __fdividef(1.f, L);
+        const float inv = L == 0.f ? 0.f : __fdividef(1.f, L);
 #pragma unroll
         for (int e = 0; e < E; ++e) a.out[bh * D + E * lane + e] = o[e] * inv;
         if (a.lse && lane == 0) a.lse[bh] = (M + __log2f(L)) * 0.6931471805599453f;
@@ -571,7 +574,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   const int heads_log2 = gc > 4 ? 3 : (gc > 2 ? 2 : (gc > 1 ? 1 : 0)), ways = DP_WARPS >> heads_log2;
   const int h = warp & ((1 << heads_log2) - 1), way = warp >> heads_log2;
   float* sums = own + PART + warp * (D + 2);  // [warp]: maximum, sum, output
-  float M = -1e30f, L = 0.f, o[E] = {};
+  float M = DP_FLOOR, L = 0.f, o[E] = {};
   if (h < gc) {
 #pragma unroll 4
     for (int k = way; k < count; k += ways) {
@@ -609,7 +612,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
   if (late_s) L = NAN;
   const size_t bh = static_cast<size_t>(ending.b) * a.Hq + head * a.g + h0 + h;
-  const float inv = __fdividef(1.f, L);
+  const float inv = L == 0.f ? 0.f : __fdividef(1.f, L);
 #pragma unroll
   for (int e = 0; e < E; ++e) a.out[bh * D + E * lane + e] = o[e] * inv;
   if (a.lse && lane == 0) a.lse[bh] = (M + __log2f(L)) * 0.6931471805599453f;
