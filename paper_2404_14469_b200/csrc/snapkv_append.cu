@@ -58,7 +58,7 @@ template <int D, bool INTERLEAVED, int TB>
 __global__ void __launch_bounds__(AP_THREADS) append_kernel(const AppendArgs a) {
   constexpr int ITEMS = D / 16;                        // of a head
   constexpr int STEP = AP_THREADS / (ITEMS * TB);      // heads in flight
-  __shared__ float cs[TB][D / 2], sn[TB][D / 2];
+  __shared__ __align__(16) float cs[TB][D / 2], sn[TB][D / 2];  // (read as float4)
   __shared__ long long src_b[TB], src_i[TB], k_to[TB], v_to[TB];  // sequence and row of the source; targets or -1
   __shared__ int live[TB];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
