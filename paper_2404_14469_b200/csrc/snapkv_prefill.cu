@@ -79,10 +79,22 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
-__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
+// Where `on`, which lanes may differ in: predicated instructions instead of branches, so that the warp stays
+// whole for the .sync.aligned ones around them.
+__device__ __forceinline__ void st_global_32_if(bool on, void* p, const uint32_t (&w)[8]) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %9, 0;\n\t"
+      "@p st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n\t}" ::"l"(p),
+      "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(static_cast<int>(on))
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_if(bool on, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(static_cast<int>(on))
+      : "memory");
 }
 
 // Wait for a copy or an MMA that is in flight, when the abort flag is set already.
@@ -411,7 +423,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       }
       u = units_s[at_unit];
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_read(at_unit));
+      mbar_arrive_if(lane == 0, bar_read(at_unit));
       if (u.most < 0) break;
       const int token = u.token0 + (SPLIT ? 0 : t * tile_tokens) + (row >> a.pack_log2);
       const int head = u.head0 + (row & ((1 << a.pack_log2) - 1));
@@ -536,7 +548,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p(t, h));
+          mbar_arrive_if(lane == 0, bar_p(t, h));
         }
       }
       // ---- the tile's result
@@ -565,7 +577,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           theirs[(D + 1) * 128] = far;
           theirs[(D + 2) * 128] = l;
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_of(1));
+          mbar_arrive_if(lane == 0, bar_of(1));
           continue;
         }
         if (ok && u.nk[1] > 0) {
@@ -589,6 +601,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         const int w = token - (u.lq - a.W);
         if (w >= 0) a.lse_obs[(static_cast<long long>(u.batch) * a.Hq + head) * a.W + w] = e;
       }
+      __syncwarp();
       // (a row per lane: 32-byte stores write whole sectors and take half of the passes through the
       // load/store unit that 16-byte ones do)
       uint32_t o[16] = {}, ahead[16] = {};
@@ -603,12 +616,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           for (int e = 0; e < 16; ++e) o[e] = ahead[e];
           if (c + 16 < D) tmem_ld16(o_at + c + 16, ahead);
         }
-        if (!mine) continue;
         if constexpr (SPLIT) {
-          if (f_their != 0.f)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              o[e] = __float_as_uint(__uint_as_float(o[e]) * f_own + theirs[(c + e) * 128] * f_their);
+          for (int e = 0; e < 16; ++e) {
+            const float x = __uint_as_float(o[e]) * f_own + theirs[(c + e) * 128] * f_their;
+            o[e] = f_their != 0.f ? __float_as_uint(x) : o[e];
+          }
         }
         uint32_t w[8];
 #pragma unroll
@@ -618,15 +631,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
           const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
           w[e] = bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t*>(&h);
         }
-        st_global_32(a.out + at * D + c, w);
+        st_global_32_if(mine, a.out + at * D + c, w);
       }
       if (ok && nk > 0) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_of(t));
+        mbar_arrive_if(lane == 0, bar_of(t));
       }
     }
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {
