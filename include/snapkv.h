@@ -589,6 +589,20 @@ snapkv_status_t snapkv_selftest_withheld_partials(const void* q_obs, const void*
                                                   int B, int Hq, int Hkv, int L, int d, int W,
                                                   void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Self-test of the waits between the blocks of snapkv_decode_paged (no counterpart in the paper).  Same arguments
+ * and work, but a partial result that another block waits for is published only when that block has given it up
+ * (after the wait limit; lower it first and restore it afterwards).  The heads of sequences whose rows are
+ * shared by several blocks become NaN, out_lse too; the others are as from snapkv_decode_paged.  The workspace is
+ * as good as before for any later call, and for further replays of a graph that this call was captured in.
+ */
+snapkv_status_t snapkv_selftest_late_partials(const void* q_cur, const void* k_pool, const void* v_pool,
+                                              const int64_t* k_strides, const int64_t* v_strides,
+                                              const int32_t* page_table, int pages_per_seq, int page_size,
+                                              int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
+                                              float* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                              void* stream);
+
 /* Number of kernel launches the last successful snapkv_compress /
  * snapkv_window_scores call of this thread enqueued (for accounting in benchmarks).
  * Host only. */

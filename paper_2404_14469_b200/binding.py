@@ -34,7 +34,7 @@ SYMBOLS = [
     "snapkv_compress_grouped", "snapkv_compress_varlen", "snapkv_varlen_workspace_size",
     "snapkv_hit_counts", "snapkv_decode_workspace_size", "snapkv_decode_attention",
     "snapkv_set_wait_limit_ns", "snapkv_selftest_stalled_scores", "snapkv_schedule_items",
-    "snapkv_selftest_withheld_partials",
+    "snapkv_selftest_withheld_partials", "snapkv_selftest_late_partials",
     "snapkv_compress_paged",
     "snapkv_shard_lse", "snapkv_lse_merge", "snapkv_shard_votes", "snapkv_gather_range",
     "snapkv_prefill_attention", "snapkv_append_paged", "snapkv_decode_paged_workspace_size", "snapkv_decode_paged",
@@ -144,6 +144,8 @@ def lib() -> ctypes.CDLL:
     L.snapkv_selftest_stalled_scores.argtypes = L.snapkv_window_scores.argtypes
     L.snapkv_selftest_withheld_partials.restype = c_int
     L.snapkv_selftest_withheld_partials.argtypes = [c_vp, c_vp, p32] + [c_int] * 6 + [c_vp, c_sz, c_vp]
+    L.snapkv_selftest_late_partials.restype = c_int
+    L.snapkv_selftest_late_partials.argtypes = L.snapkv_decode_paged.argtypes
     _lib = L
     return L
 
@@ -486,6 +488,22 @@ def snapkv_selftest_withheld_partials(q_obs, k, workspace, seq_lens=None):
     code = lib().snapkv_selftest_withheld_partials(q_obs.data_ptr(), k.data_ptr(), lens, B, Hq, Hkv, L, d, W,
                                                    workspace.data_ptr(), workspace.numel(), _stream_ptr())
     _check(code, "snapkv_selftest_withheld_partials")
+
+
+def snapkv_selftest_late_partials(q_cur, k_pool, v_pool, page_table, seq_lens, workspace):
+    """snapkv_decode_paged whose blocks publish partial results only when they have been given up (time-out
+    self-test).  Returns (out, lse) as that call does, NaN in what several blocks share."""
+    _dev_bf16(q_cur, "q_cur")
+    (B, Hq, d), (pages, Hc, page, _) = q_cur.shape, k_pool.shape
+    out = torch.empty(B, Hq, d, dtype=torch.float32, device=q_cur.device)
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=q_cur.device)
+    strides = [(ctypes.c_int64 * 3)(*x.stride()[:3]) for x in (k_pool, v_pool)]
+    code = lib().snapkv_selftest_late_partials(q_cur.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *strides,
+                                               page_table.data_ptr(), page_table.shape[1], page, pages,
+                                               seq_lens.data_ptr(), B, Hq, Hc, d, out.data_ptr(), lse.data_ptr(),
+                                               workspace.data_ptr(), workspace.numel(), _stream_ptr())
+    _check(code, "snapkv_selftest_late_partials")
+    return out, lse
 
 
 def snapkv_pool_topk(vote, pool_kernel: int, pool_type: int, ksel: int, out_idx=None,

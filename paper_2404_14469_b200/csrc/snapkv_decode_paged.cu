@@ -11,9 +11,11 @@
 // unnormalised output) per share; the block folds those of its own warps once, at its end, and the
 // block that has the unit's last share those of the blocks in front of it, in the order of the
 // shares: same bits every run.  It waits (bounded) for a flag beside each partial.  The flags are the
-// call's own 64-bit number, not a count, so that nothing has to be cleared in front of the call; they
-// are taken back by who read them.  A block waits for blocks of lower numbers alone, which wait for
-// nothing before they have published: they need not be resident together.
+// call's own 64-bit number, not a count, so that nothing has to be cleared in front of the call.  A replayed
+// graph makes the same call again, so none may be left behind: who has read a flag clears it; who gives a
+// flag up leaves the number's complement there, which tells the publisher, who comes later, to clear it.
+// A block waits for blocks of lower numbers alone, which wait for nothing before they have published: they
+// need not be resident together.
 // What lies behind a sequence's last row may be anything: scores there are replaced and the values
 // zeroed in registers, in a unit's last tile alone.
 #include <cuda.h>
@@ -41,6 +43,8 @@ constexpr int DP_BOX_ROWS = 16;               // rows per copy: a page holds a w
 constexpr int DP_HEADS = 8;                   // query heads of a unit
 constexpr int DP_THREADS = DP_WARPS * 32;
 constexpr int DP_MAX_GRID = MAX_GRID;
+// A block's last two threads publish, its first ones wait: up to one per block in front.
+static_assert(DP_MAX_GRID <= DP_THREADS - 32, "a warp that publishes does not wait");
 // What a unit costs a warp beside its tiles (queries to fetch, a result to reduce and write), in tiles:
 // shares are equal in tiles and units.  (64 sequences of 20 to 300 rows: 14.9 us with 1, 14.0 with 2,
 // 13.8 with 3; of 30 to 8000 rows 62.7, 61.9, 62.1.)
@@ -64,7 +68,8 @@ struct DecodePagedArgs {
   // workspace: [2 * grid] flags, then as many partials of DP_HEADS * (D + 2) floats: of the unit that
   // a block's shares begin inside, of the last one that they begin
   unsigned long long* flags;
-  unsigned long long call;  // what marks a partial of this call as written
+  unsigned long long call;  // what marks a partial of this call as written; its complement: as given up
+  bool late;                // self-test: partials are published when they have been given up
   float* partials;
 };
 
@@ -79,8 +84,10 @@ __device__ __forceinline__ unsigned long long ld_flag(const unsigned long long* 
   asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
   return v;
 }
-__device__ __forceinline__ void st_flag(unsigned long long* p, unsigned long long v) {
-  asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
+__device__ __forceinline__ unsigned long long swap_flag(unsigned long long* p, unsigned long long v) {
+  unsigned long long was;
+  asm volatile("atom.acq_rel.gpu.global.exch.b64 %0, [%1], %2;" : "=l"(was) : "l"(p), "l"(v) : "memory");
+  return was;
 }
 
 // (a 64-bit division takes several times as long as one of 32 bits)
@@ -176,7 +183,6 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   pdl_wait();  // everything above touched this block's shared memory only
 
   // ---- the warps' shares.  Every thread adds up the pieces of its run of sequences.
-  if (threadIdx.x < 2) a.flags[2 * blockIdx.x + threadIdx.x] = 0;  // (what a wait that gave up may have left)
   if (threadIdx.x == 0) {
     late_s = publish_s[0] = publish_s[1] = 0;
     ending_s.b = -1;
@@ -548,9 +554,15 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     }
   }
   __syncthreads();
-  if (threadIdx.x < 2 && publish_s[threadIdx.x]) {
+  if (const int i = DP_THREADS - 1 - static_cast<int>(threadIdx.x); i < 2 && publish_s[i]) {
+    unsigned long long* flag = a.flags + 2 * blockIdx.x + i;
+    if (a.late) {
+      const unsigned long long t0 = globaltimer_ns();
+      while (ld_flag(flag) != ~a.call && globaltimer_ns() - t0 < 4 * a.wait_ns) {
+      }
+    }
     __threadfence();
-    st_flag(a.flags + 2 * blockIdx.x + threadIdx.x, a.call);
+    if (swap_flag(flag, a.call) == ~a.call) *flag = 0;  // nobody waits any more
   }
   const Left ending = ending_s;
   if (ending.b < 0) return;
@@ -562,12 +574,12 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   if (static_cast<int>(threadIdx.x) < count) {
     unsigned long long* flag = a.flags + slot_of(threadIdx.x);
     const unsigned long long t0 = globaltimer_ns();
-    while (ld_flag(flag) != a.call)
-      if (globaltimer_ns() - t0 > a.wait_ns) {
-        late_s = 1;
-        break;
-      }
-    *flag = 0;
+    bool there;
+    while (!(there = ld_flag(flag) == a.call) && globaltimer_ns() - t0 <= a.wait_ns) {
+    }
+    // read, or given up: unless it came in that moment, the publisher clears it
+    if (there || swap_flag(flag, ~a.call) == a.call) *flag = 0;
+    else late_s = 1;
   }
   __syncthreads();
   // DP_WARPS / 2^x warps per head, each with every so many-th partial; then theirs and the block's own
@@ -619,17 +631,20 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 }
 
 // A number that no other call has: partials of an earlier call, of another process in the same memory
-// or of whatever was there do not pass for this call's.
+// or of whatever was there do not pass for this call's.  (The SplitMix64 generator of Steele, Lea and Flood, 2014: a
+// counter with an odd step, mixed one to one.)
 unsigned long long call_number() {
   static const unsigned long long seed =
       static_cast<unsigned long long>(std::chrono::system_clock::now().time_since_epoch().count()) ^
       (static_cast<unsigned long long>(getpid()) << 40);
   static std::atomic<unsigned long long> calls{0};
-  unsigned long long x = seed + ++calls * 0x9e3779b97f4a7c15ull;  // (odd: a step through all 64-bit numbers)
-  x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;                    // mixed one to one
-  x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
-  x ^= x >> 31;
-  return x ? x : 1;
+  for (;;) {
+    unsigned long long x = seed + ++calls * 0x9e3779b97f4a7c15ull;  // (odd: a step through all 64-bit numbers)
+    x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;                    // mixed one to one
+    x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+    x ^= x >> 31;
+    if (x != 0 && x != ~0ull) return x;  // (0 is a cleared flag, and must not be a complement either)
+  }
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -672,13 +687,13 @@ extern "C" size_t snapkv_decode_paged_workspace_size(int B, int Hq, int Hc, int 
          align256(static_cast<size_t>(2) * DP_MAX_GRID * DP_HEADS * (d + 2) * sizeof(float));
 }
 
-extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_pool, const void* v_pool,
-                                               const int64_t* k_strides, const int64_t* v_strides,
-                                               const int32_t* page_table, int pages_per_seq, int page_size,
-                                               int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
-                                               float* out, float* out_lse, void* workspace, size_t workspace_bytes,
-                                               void* stream) {
-  using namespace snapkv;
+namespace snapkv {
+namespace {
+
+snapkv_status_t decode_paged(const void* q_cur, const void* k_pool, const void* v_pool, const int64_t* k_strides,
+                             const int64_t* v_strides, const int32_t* page_table, int pages_per_seq, int page_size,
+                             int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d, float* out,
+                             float* out_lse, void* workspace, size_t workspace_bytes, void* stream, bool late) {
   if (B < 1 || Hq < 1 || Hc < 1 || Hq % Hc != 0 || d < 1 || pages_per_seq < 1 || page_size < 1 || num_pages < 1 ||
       page_size % DP_BOX_ROWS != 0)
     return SNAPKV_ERR_INVALID_ARG;
@@ -711,9 +726,33 @@ extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_
   a.out = out, a.lse = out_lse;
   a.flags = static_cast<unsigned long long*>(workspace);
   a.call = call_number();
+  a.late = late;
   a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(2 * DP_MAX_GRID * sizeof(unsigned long long)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto f = d == 128 ? (a.g <= 2 ? launch_decode_paged<128, 2> : (a.g <= 4 ? launch_decode_paged<128, 4> : launch_decode_paged<128, 8>))
                     : (a.g <= 2 ? launch_decode_paged<64, 2> : (a.g <= 4 ? launch_decode_paged<64, 4> : launch_decode_paged<64, 8>));
   return f(tmK, tmV, a, s) == cudaSuccess ? SNAPKV_OK : SNAPKV_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace snapkv
+
+extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_pool, const void* v_pool,
+                                               const int64_t* k_strides, const int64_t* v_strides,
+                                               const int32_t* page_table, int pages_per_seq, int page_size,
+                                               int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
+                                               float* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                               void* stream) {
+  return snapkv::decode_paged(q_cur, k_pool, v_pool, k_strides, v_strides, page_table, pages_per_seq, page_size,
+                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream, false);
+}
+
+extern "C" snapkv_status_t snapkv_selftest_late_partials(const void* q_cur, const void* k_pool, const void* v_pool,
+                                                         const int64_t* k_strides, const int64_t* v_strides,
+                                                         const int32_t* page_table, int pages_per_seq, int page_size,
+                                                         int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc,
+                                                         int d, float* out, float* out_lse, void* workspace,
+                                                         size_t workspace_bytes, void* stream) {
+  return snapkv::decode_paged(q_cur, k_pool, v_pool, k_strides, v_strides, page_table, pages_per_seq, page_size,
+                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream, true);
 }
