@@ -603,6 +603,30 @@ snapkv_status_t snapkv_selftest_late_partials(const void* q_cur, const void* k_p
                                               float* out, float* out_lse, void* workspace, size_t workspace_bytes,
                                               void* stream);
 
+/*
+ * Self-tests of the waits for copies in snapkv_prefill_attention and snapkv_decode_paged (no counterpart in the paper):
+ * copies that are never made.  Lower the wait limit first and restore it afterwards; both calls take a few times
+ * the limit.
+ *   snapkv_selftest_lost_keys: same arguments, and the number of a work unit of the launch (of each launch, where there are
+ *     several) whose first keys never come.  The unit's rows become NaN (out, out_lse and lse_obs), and so do those
+ *     of the units, two at most, that its block has taken over by then; all other rows are as from
+ *     snapkv_prefill_attention.
+ *     Nothing happens where there is no such unit or where it sees no key.  unit >= 0.
+ *   snapkv_selftest_lost_rows: same arguments; no warp's first rows ever come.  Sequences with rows become NaN.
+ */
+snapkv_status_t snapkv_selftest_lost_keys(const void* q, const void* k, const void* v,
+                                          const int64_t* q_strides, const int64_t* k_strides,
+                                          const int64_t* v_strides, const int32_t* q_lens,
+                                          const int32_t* k_lens, const int64_t* q_starts,
+                                          const int64_t* k_starts, int B, int Hq, int Hkv, int d, int W,
+                                          void* out, float* out_lse, float* lse_obs, int unit, void* stream);
+snapkv_status_t snapkv_selftest_lost_rows(const void* q_cur, const void* k_pool, const void* v_pool,
+                                          const int64_t* k_strides, const int64_t* v_strides,
+                                          const int32_t* page_table, int pages_per_seq, int page_size,
+                                          int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
+                                          float* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                          void* stream);
+
 /* Number of kernel launches the last successful snapkv_compress /
  * snapkv_window_scores call of this thread enqueued (for accounting in benchmarks).
  * Host only. */

@@ -34,7 +34,8 @@ SYMBOLS = [
     "snapkv_compress_grouped", "snapkv_compress_varlen", "snapkv_varlen_workspace_size",
     "snapkv_hit_counts", "snapkv_decode_workspace_size", "snapkv_decode_attention",
     "snapkv_set_wait_limit_ns", "snapkv_selftest_stalled_scores", "snapkv_schedule_items",
-    "snapkv_selftest_withheld_partials", "snapkv_selftest_late_partials",
+    "snapkv_selftest_withheld_partials", "snapkv_selftest_late_partials", "snapkv_selftest_lost_keys",
+    "snapkv_selftest_lost_rows",
     "snapkv_compress_paged",
     "snapkv_shard_lse", "snapkv_lse_merge", "snapkv_shard_votes", "snapkv_gather_range",
     "snapkv_prefill_attention", "snapkv_append_paged", "snapkv_decode_paged_workspace_size", "snapkv_decode_paged",
@@ -146,6 +147,10 @@ def lib() -> ctypes.CDLL:
     L.snapkv_selftest_withheld_partials.argtypes = [c_vp, c_vp, p32] + [c_int] * 6 + [c_vp, c_sz, c_vp]
     L.snapkv_selftest_late_partials.restype = c_int
     L.snapkv_selftest_late_partials.argtypes = L.snapkv_decode_paged.argtypes
+    L.snapkv_selftest_lost_rows.restype = c_int
+    L.snapkv_selftest_lost_rows.argtypes = L.snapkv_decode_paged.argtypes
+    L.snapkv_selftest_lost_keys.restype = c_int
+    L.snapkv_selftest_lost_keys.argtypes = L.snapkv_prefill_attention.argtypes[:-1] + [c_int, c_vp]
     _lib = L
     return L
 
@@ -490,20 +495,44 @@ def snapkv_selftest_withheld_partials(q_obs, k, workspace, seq_lens=None):
     _check(code, "snapkv_selftest_withheld_partials")
 
 
-def snapkv_selftest_late_partials(q_cur, k_pool, v_pool, page_table, seq_lens, workspace):
-    """snapkv_decode_paged whose blocks publish partial results only when they have been given up (time-out
-    self-test).  Returns (out, lse) as that call does, NaN in what several blocks share."""
+def _paged_selftest(name, q_cur, k_pool, v_pool, page_table, seq_lens, workspace):
     _dev_bf16(q_cur, "q_cur")
     (B, Hq, d), (pages, Hc, page, _) = q_cur.shape, k_pool.shape
     out = torch.empty(B, Hq, d, dtype=torch.float32, device=q_cur.device)
     lse = torch.empty(B, Hq, dtype=torch.float32, device=q_cur.device)
     strides = [(ctypes.c_int64 * 3)(*x.stride()[:3]) for x in (k_pool, v_pool)]
-    code = lib().snapkv_selftest_late_partials(q_cur.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *strides,
-                                               page_table.data_ptr(), page_table.shape[1], page, pages,
-                                               seq_lens.data_ptr(), B, Hq, Hc, d, out.data_ptr(), lse.data_ptr(),
-                                               workspace.data_ptr(), workspace.numel(), _stream_ptr())
-    _check(code, "snapkv_selftest_late_partials")
+    code = getattr(lib(), name)(q_cur.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *strides, page_table.data_ptr(),
+                                page_table.shape[1], page, pages, seq_lens.data_ptr(), B, Hq, Hc, d, out.data_ptr(),
+                                lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr())
+    _check(code, name)
     return out, lse
+
+
+def snapkv_selftest_late_partials(q_cur, k_pool, v_pool, page_table, seq_lens, workspace):
+    """snapkv_decode_paged whose blocks publish partial results only when they have been given up (time-out
+    self-test).  Returns (out, lse) as that call does, NaN in what several blocks share."""
+    return _paged_selftest("snapkv_selftest_late_partials", q_cur, k_pool, v_pool, page_table, seq_lens, workspace)
+
+
+def snapkv_selftest_lost_rows(q_cur, k_pool, v_pool, page_table, seq_lens, workspace):
+    """snapkv_decode_paged whose warps wait for first rows that never come (time-out self-test).  Returns (out, lse),
+    NaN for sequences with rows."""
+    return _paged_selftest("snapkv_selftest_lost_rows", q_cur, k_pool, v_pool, page_table, seq_lens, workspace)
+
+
+def snapkv_selftest_lost_keys(q, k, v, q_lens, unit: int, k_lens=None, window: int = 0):
+    """snapkv_prefill_attention of dense q, k, v, where the first keys of a work unit never come (time-out self-test).
+    Returns (out, lse, lse_obs or None), NaN in the unit's rows and in those that its block had taken over."""
+    (T, Hq, d), B = q.shape, len(q_lens)
+    _dev_bf16(q, "q"), _dev_bf16(k, "k"), _dev_bf16(v, "v")
+    out, lse = torch.empty_like(q), torch.empty(T, Hq, dtype=torch.float32, device=q.device)
+    obs = torch.empty(B, Hq, window, dtype=torch.float32, device=q.device) if window else None
+    lens = lambda x: None if x is None else (ctypes.c_int32 * B)(*x)
+    code = lib().snapkv_selftest_lost_keys(q.data_ptr(), k.data_ptr(), v.data_ptr(), None, None, None, lens(q_lens),
+                                           lens(k_lens), None, None, B, Hq, k.shape[1], d, window, out.data_ptr(),
+                                           lse.data_ptr(), obs.data_ptr() if window else None, unit, _stream_ptr())
+    _check(code, "snapkv_selftest_lost_keys")
+    return out, lse, obs
 
 
 def snapkv_pool_topk(vote, pool_kernel: int, pool_type: int, ksel: int, out_idx=None,

@@ -53,6 +53,9 @@ constexpr int DP_UNIT_COST = 2;
 // that scores of minus infinity weigh nothing and minus infinity is not subtracted from itself.
 constexpr float DP_FLOOR = -1e38f;
 
+// Self-tests: partials are published when they have been given up; no warp's first tile ever comes.
+constexpr int DP_LATE = 1, DP_LOST = 2;
+
 constexpr int dp_tile_rows(int D) { return DP_STAGE_BYTES / (4 * D); }
 
 struct DecodePagedArgs {
@@ -69,7 +72,7 @@ struct DecodePagedArgs {
   // a block's shares begin inside, of the last one that they begin
   unsigned long long* flags;
   unsigned long long call;  // what marks a partial of this call as written; its complement: as given up
-  bool late;                // self-test: partials are published when they have been given up
+  int selftest;             // DP_LATE, DP_LOST or 0
   float* partials;
 };
 
@@ -283,9 +286,10 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       }
   };
   int issued = 0;
+  const int lost = a.selftest == DP_LOST ? 0 : -1;
   auto request = [&] {  // K and V of the tile at hand, then on to the next
     if (!tiles_left) return;
-    if (lane == 0) {
+    if (lane == 0 && issued != lost) {
       const uint32_t dst = ring + (issued % DP_STAGES) * DP_STAGE_BYTES, bs = bar + 8u * (issued % DP_STAGES);
       const int head = ahead.unit / a.chunks;
       mbar_expect_tx(bs, DP_STAGE_BYTES);
@@ -556,7 +560,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   __syncthreads();
   if (const int i = DP_THREADS - 1 - static_cast<int>(threadIdx.x); i < 2 && publish_s[i]) {
     unsigned long long* flag = a.flags + 2 * blockIdx.x + i;
-    if (a.late) {
+    if (a.selftest == DP_LATE) {
       const unsigned long long t0 = globaltimer_ns();
       while (ld_flag(flag) != ~a.call && globaltimer_ns() - t0 < 4 * a.wait_ns) {
       }
@@ -693,7 +697,7 @@ namespace {
 snapkv_status_t decode_paged(const void* q_cur, const void* k_pool, const void* v_pool, const int64_t* k_strides,
                              const int64_t* v_strides, const int32_t* page_table, int pages_per_seq, int page_size,
                              int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d, float* out,
-                             float* out_lse, void* workspace, size_t workspace_bytes, void* stream, bool late) {
+                             float* out_lse, void* workspace, size_t workspace_bytes, void* stream, int selftest) {
   if (B < 1 || Hq < 1 || Hc < 1 || Hq % Hc != 0 || d < 1 || pages_per_seq < 1 || page_size < 1 || num_pages < 1 ||
       page_size % DP_BOX_ROWS != 0)
     return SNAPKV_ERR_INVALID_ARG;
@@ -726,7 +730,7 @@ snapkv_status_t decode_paged(const void* q_cur, const void* k_pool, const void* 
   a.out = out, a.lse = out_lse;
   a.flags = static_cast<unsigned long long*>(workspace);
   a.call = call_number();
-  a.late = late;
+  a.selftest = selftest;
   a.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + align256(2 * DP_MAX_GRID * sizeof(unsigned long long)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto f = d == 128 ? (a.g <= 2 ? launch_decode_paged<128, 2> : (a.g <= 4 ? launch_decode_paged<128, 4> : launch_decode_paged<128, 8>))
@@ -744,7 +748,7 @@ extern "C" snapkv_status_t snapkv_decode_paged(const void* q_cur, const void* k_
                                                float* out, float* out_lse, void* workspace, size_t workspace_bytes,
                                                void* stream) {
   return snapkv::decode_paged(q_cur, k_pool, v_pool, k_strides, v_strides, page_table, pages_per_seq, page_size,
-                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream, false);
+                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream, 0);
 }
 
 extern "C" snapkv_status_t snapkv_selftest_late_partials(const void* q_cur, const void* k_pool, const void* v_pool,
@@ -754,5 +758,17 @@ extern "C" snapkv_status_t snapkv_selftest_late_partials(const void* q_cur, cons
                                                          int d, float* out, float* out_lse, void* workspace,
                                                          size_t workspace_bytes, void* stream) {
   return snapkv::decode_paged(q_cur, k_pool, v_pool, k_strides, v_strides, page_table, pages_per_seq, page_size,
-                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream, true);
+                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream,
+                              snapkv::DP_LATE);
+}
+
+extern "C" snapkv_status_t snapkv_selftest_lost_rows(const void* q_cur, const void* k_pool, const void* v_pool,
+                                                     const int64_t* k_strides, const int64_t* v_strides,
+                                                     const int32_t* page_table, int pages_per_seq, int page_size,
+                                                     int num_pages, const int32_t* seq_lens, int B, int Hq, int Hc, int d,
+                                                     float* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                                     void* stream) {
+  return snapkv::decode_paged(q_cur, k_pool, v_pool, k_strides, v_strides, page_table, pages_per_seq, page_size,
+                              num_pages, seq_lens, B, Hq, Hc, d, out, out_lse, workspace, workspace_bytes, stream,
+                              snapkv::DP_LOST);
 }

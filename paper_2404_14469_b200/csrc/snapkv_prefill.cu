@@ -39,6 +39,9 @@ constexpr int PF_MAX_SEQS = 32;   // sequences that share a launch
 constexpr int PF_THREADS = 320;
 constexpr int PF_UNITS = 4;       // units that the TMA thread may be ahead
 constexpr int PF_KEYS = 128;      // keys per tile
+// When a wait has given up, the block's other roles wait for the TMA thread to tell which units are left: it
+// waits first for its queries, up to eight tiles, an answer and two units' places.  In wait limits.
+constexpr int PF_PATIENCE = 16;
 // A row's reference is 2^10 (PF_ROOM) above the keys that it was taken from, and the row takes a new one
 // when 64 of its weights add up to more than 64 (PF_FAR).  So the sums are at most what a running maximum
 // gives, (Lk + 64) and (Lk + 64) max|v|, and logits may rise by 2^10 to 2^16 without a new reference.  (The
@@ -67,6 +70,7 @@ struct PrefillArgs {
   int head_packs;      // Hq >> pack_log2
   float c2;            // log2(e) / sqrt(d)
   unsigned long long wait_ns;
+  int lost;            // self-test: the unit whose first key tile never comes, else -1
   __nv_bfloat16* out;
   float *lse, *lse_obs;
 };
@@ -267,12 +271,16 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         if (ended) break;
         if (u.most == 0) continue;
         const int kv = u.head0 / a.g;
+        bool lost = i == a.lost;
         auto load = [&](const CUtensorMap* m, int j) {
           const int s = fill % STAGES;
           if (!mbar_wait_thread(bar_empty(s), (fill / STAGES & 1) ^ 1, abort_s, 1)) return false;
-          mbar_expect_tx(bar_full(s), TILE);
-          for (int c = 0; c < COLS; ++c)
-            tma_load_3d(kv_s + s * TILE + c * PF_BLOCK, m, bar_full(s), c * 64, j * PF_KEYS, kv);
+          if (!lost) {
+            mbar_expect_tx(bar_full(s), TILE);
+            for (int c = 0; c < COLS; ++c)
+              tma_load_3d(kv_s + s * TILE + c * PF_BLOCK, m, bar_full(s), c * 64, j * PF_KEYS, kv);
+          }
+          lost = false;
           ++fill;
           return true;
         };
@@ -350,11 +358,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
         ++npv[t];
         return true;
       };
-      for (int r = 0; ok; ++r) {
+      int r = 0;  // units read
+      while (ok) {
         ok = mbar_wait_thread(bar_there(r % PF_UNITS), r / PF_UNITS & 1, abort_s, 11);
         if (!ok) break;
         u = units_s[r % PF_UNITS];
-        mbar_arrive(bar_read(r % PF_UNITS));
+        mbar_arrive(bar_read(r++ % PF_UNITS));
         if (u.most < 0) break;
         if (u.most == 0) continue;
         ok = mbar_wait_thread(bar_qf, nq++ & 1, abort_s, 7);
@@ -401,6 +410,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       if (*abort_s != 0) {
         tc_commit(bar_drain);
         drain(bar_drain, 0, a.wait_ns);
+        // units that the softmax warps have still to fill: their places become free without this role
+        const unsigned long long t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < PF_PATIENCE * a.wait_ns) {
+          if (mbar_try_wait(bar_there(r % PF_UNITS), r / PF_UNITS & 1)) mbar_arrive(bar_read(r++ % PF_UNITS));
+          else if (*closed_s >= 0 && r >= *closed_s) break;
+        }
       }
     }
   } else {
@@ -416,10 +431,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const PrefillArgs a, con
       ok = ok && mbar_wait_warp(bar_there(at_unit), r / PF_UNITS & 1, abort_s, 11);
       if (!ok) {  // a wait gave up: what units there still are become NaN, once it is known how many
         const unsigned long long t0 = globaltimer_ns();
-        while (__any_sync(0xffffffffu, *closed_s < 0 && globaltimer_ns() - t0 < 8 * a.wait_ns)) {
-          if (__all_sync(0xffffffffu, mbar_try_wait(bar_there(at_unit), r / PF_UNITS & 1))) break;
+        bool there = false;
+        while (!(there = __all_sync(0xffffffffu, mbar_try_wait(bar_there(at_unit), r / PF_UNITS & 1)))) {
+          const int closed = *closed_s;
+          if (__any_sync(0xffffffffu, (closed >= 0 && r >= closed) || globaltimer_ns() - t0 > PF_PATIENCE * a.wait_ns)) break;
         }
-        if (!__all_sync(0xffffffffu, mbar_try_wait(bar_there(at_unit), r / PF_UNITS & 1))) break;
+        if (!there) break;
       }
       u = units_s[at_unit];
       __syncwarp();
@@ -714,13 +731,14 @@ cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ,
 }  // namespace
 }  // namespace snapkv
 
-extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const void* v,
-                                                    const int64_t* q_strides, const int64_t* k_strides,
-                                                    const int64_t* v_strides, const int32_t* q_lens,
-                                                    const int32_t* k_lens, const int64_t* q_starts,
-                                                    const int64_t* k_starts, int B, int Hq, int Hkv, int d, int W,
-                                                    void* out, float* out_lse, float* lse_obs, void* stream) {
-  using namespace snapkv;
+namespace snapkv {
+namespace {
+
+snapkv_status_t prefill_attention(const void* q, const void* k, const void* v, const int64_t* q_strides,
+                                  const int64_t* k_strides, const int64_t* v_strides, const int32_t* q_lens,
+                                  const int32_t* k_lens, const int64_t* q_starts, const int64_t* k_starts, int B, int Hq,
+                                  int Hkv, int d, int W, void* out, float* out_lse, float* lse_obs, int lost,
+                                  void* stream) {
   if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || d < 1 || W < 0 || !q_lens) return SNAPKV_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || W > 128 || Hq > 65535) return SNAPKV_ERR_UNSUPPORTED;
   if (!q || !k || !v || !out || (W > 0) != (lse_obs != nullptr)) return SNAPKV_ERR_INVALID_ARG;
@@ -749,6 +767,7 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
   a.head_packs = Hq >> a.pack_log2;
   a.c2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
   a.wait_ns = wait_limit_setting();
+  a.lost = lost;
   a.out = static_cast<__nv_bfloat16*>(out);
   a.lse = out_lse, a.lse_obs = lse_obs;
   if (queries == 0) return SNAPKV_OK;
@@ -786,4 +805,28 @@ extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k
     if (e != cudaSuccess) return SNAPKV_ERR_CUDA;
   }
   return SNAPKV_OK;
+}
+
+}  // namespace
+}  // namespace snapkv
+
+extern "C" snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const void* v,
+                                                    const int64_t* q_strides, const int64_t* k_strides,
+                                                    const int64_t* v_strides, const int32_t* q_lens,
+                                                    const int32_t* k_lens, const int64_t* q_starts,
+                                                    const int64_t* k_starts, int B, int Hq, int Hkv, int d, int W,
+                                                    void* out, float* out_lse, float* lse_obs, void* stream) {
+  return snapkv::prefill_attention(q, k, v, q_strides, k_strides, v_strides, q_lens, k_lens, q_starts, k_starts, B, Hq,
+                                   Hkv, d, W, out, out_lse, lse_obs, -1, stream);
+}
+
+extern "C" snapkv_status_t snapkv_selftest_lost_keys(const void* q, const void* k, const void* v,
+                                                     const int64_t* q_strides, const int64_t* k_strides,
+                                                     const int64_t* v_strides, const int32_t* q_lens,
+                                                     const int32_t* k_lens, const int64_t* q_starts,
+                                                     const int64_t* k_starts, int B, int Hq, int Hkv, int d, int W,
+                                                     void* out, float* out_lse, float* lse_obs, int unit, void* stream) {
+  if (unit < 0) return SNAPKV_ERR_INVALID_ARG;
+  return snapkv::prefill_attention(q, k, v, q_strides, k_strides, v_strides, q_lens, k_lens, q_starts, k_starts, B, Hq,
+                                   Hkv, d, W, out, out_lse, lse_obs, unit, stream);
 }

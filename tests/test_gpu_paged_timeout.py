@@ -87,3 +87,21 @@ def test_a_replayed_graph_never_takes_the_partials_of_an_earlier_replay():
     # the workspace is as good as before
     again = sk.snapkv_decode_paged(*case, ws)
     assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+
+
+@pytest.mark.parametrize("lens,Hq,Hc,d", [([20000], 8, 2, 128), ([300, 0, 5, 4000], 20, 2, 64), ([1] * 30, 1, 1, 128)])
+def test_rows_that_never_come(lens, Hq, Hc, d):
+    case = _case(lens, Hq, Hc, d)
+    want = sk.snapkv_decode_paged(*case)
+    ws = torch.full_like(want[2], 255)
+    with _Limit():
+        t0 = time.perf_counter()
+        out, lse = sk.snapkv_selftest_lost_rows(*case, ws)
+        torch.cuda.synchronize()
+        took = time.perf_counter() - t0
+    assert 0.015 < took < 2.0
+    some = torch.tensor(lens, device="cuda") > 0
+    assert torch.isnan(out[some]).all() and torch.isnan(lse[some]).all()
+    assert not out[~some].any() and (lse[~some] == -float("inf")).all()
+    again = sk.snapkv_decode_paged(*case, ws)
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
