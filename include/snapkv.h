@@ -406,12 +406,15 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
  *   lse_obs      fp32 device, dense [B, Hq, W]: the same of each sequence's last W queries; NULL with
  *                W = 0.  W <= 128, and with W > 0 every sequence needs W queries.
  * No sequence may begin or end behind token 2^30.
- * A query that sees no key, or whose scores are all minus infinity, gets zeros and minus infinity.  Rows of q, out and out_lse that belong to no
- * sequence are not touched; a sequence's keys and values reach its own queries only, whatever they hold.
+ * A query that sees no key, or whose scores are all minus infinity, gets zeros and minus infinity.  Rows of
+ * q, out and out_lse that belong to no sequence are not touched; a sequence's keys and values reach its own
+ * queries only, whatever they hold.
  * (Inside a sequence an infinity or NaN in a VALUE row may reach queries in front of it, too.)
  * Products of bf16 accumulated in fp32, softmax statistics in fp32, probabilities rounded to bf16 for
  * the product with V (their sum is taken before).  The sum over the values is divided last: results are
- * right as long as (Lk + 64) max|v| is a number of fp32.  Results are reproducible from run to run.  The host arrays are read during the call.  No workspace; one launch for every 32 sequences.
+ * right as long as (Lk + 64) max|v| is a number of fp32.  Results are reproducible from run to run.
+ * (What else is in the batch may change the order of a sequence's sums, and so its last bits.)  The host
+ * arrays are read during the call.  No workspace; one launch for every 32 sequences.
  * A kernel wait that exceeds its limit makes the affected rows NaN.
  */
 snapkv_status_t snapkv_prefill_attention(const void* q, const void* k, const void* v,
