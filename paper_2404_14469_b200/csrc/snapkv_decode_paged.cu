@@ -496,7 +496,7 @@ decode_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   // ---- the block's partials in the order of its shares: entry 2 w + {0, 1} is what warp w left.  A
   // unit's are consecutive: where it begins (or the block does), then one per warp until it ends.
   // A warp folds a head of a unit.  From here on the code runs once, so it is bound by fetching
-  // instructions: rolled loops (for one sequence of 777 rows the call takes 9.5 us, 13.2 with unrolled ones).
+  // instructions: rolled loops (for one sequence of 777 rows the call takes 9.6 us, 13.2 with unrolled ones).
   __syncthreads();
   float* own = reinterpret_cast<float*>(smem);  // the rings are idle: this block's part of a unit that ends here
   constexpr int E = D / 32;  // elements of a head per lane

@@ -701,7 +701,7 @@ cudaError_t run_set(const PrefillCall& c, PrefillArgs a, const CUtensorMap& tmQ,
   using u64 = unsigned long long;
   PrefillSeqs<MAPS> seqs = {};
   // One tile per unit and its keys in two halves where that leaves every unit an SM of its own: the
-  // chain is half as long (a 1K prompt of four heads of 64: 12.4 us; with two tiles per unit 17.9, with one 15.1).
+  // chain is half as long (a 1K prompt of four heads of 64: 12.5 us; with two tiles per unit 17.9, with one 15.1).
   long long tiles = 0;
   for (int i = 0; i < n; ++i) tiles += (span[i].lq + (128ll >> a.pack_log2) - 1) / (128 >> a.pack_log2) * a.head_packs;
   const bool split = tiles <= sm_count();
