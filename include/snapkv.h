@@ -412,7 +412,8 @@ snapkv_status_t snapkv_compress_paged(const void* q_obs, const void* k_pool, con
  * (Inside a sequence an infinity or NaN in a VALUE row may reach queries in front of it, too.)
  * Products of bf16 accumulated in fp32, softmax statistics in fp32, probabilities rounded to bf16 for
  * the product with V (their sum is taken before).  The sum over the values is divided last: results are
- * right as long as (Lk + 64) max|v| is a number of fp32.  Results are reproducible from run to run.
+ * right as long as (Lk + 64) max|v| is a number of fp32.  A key that weighs less than 2^-115 of a row's
+ * heaviest may count as nothing.  Results are reproducible from run to run.
  * (What else is in the batch may change the order of a sequence's sums, and so its last bits.)  The host
  * arrays are read during the call.  No workspace; one launch for every 32 sequences.
  * A kernel wait that exceeds its limit makes the affected rows NaN.
